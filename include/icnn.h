@@ -47,7 +47,10 @@ typedef enum {
     ICNN_E_LAUNCH = -6       /* the HIP runtime refused a launch                  */
 } icnn_status;
 
-typedef enum { ICNN_U8 = 0, ICNN_S8 = 1, ICNN_S32 = 2 } icnn_dtype;
+typedef enum {
+    ICNN_U8 = 0, ICNN_S8 = 1, ICNN_S32 = 2,
+    ICNN_F32 = 3, ICNN_F16 = 4, ICNN_BF16 = 5   /* streams of the feed-forward operators only */
+} icnn_dtype;
 
 typedef enum {
     ICNN_OUT_BRELU_U8 = 0,   /* clamp to [0, bound_q], store uint8                */
@@ -452,13 +455,15 @@ int iconv2d_chain_split(int32_t n_layers, const icnn_conv_desc *const *descs, in
  * and again, whose cost on the host is then one call's marshalling and not n.  Which fields a kind reads, in the order of
  * the entry point's own arguments: d its descriptors, i its integers, p its device pointers (absent ones NULL);
  * ICNN_CALL_CHAIN: i[0] layers, list[0..2] the host arrays descs, w_packed and bias, p[0] = x, p[1] = y;
+ * the feed-forward operators (ICNN_CALL_RMS_NORM and those after it): list[0] the descriptor;
  * ICNN_CALL_TRIPLE: i[0] lanes; ICNN_CALL_TRIPLE_PC: list[0..2] the channel parameters pc2_packed, pc3_packed and pc1_packed, i, p and d as ICNN_CALL_TRIPLE.
  */
 typedef enum {
     ICNN_CALL_CONV = 0, ICNN_CALL_CONV_PC = 1, ICNN_CALL_DUAL = 2, ICNN_CALL_DUAL_PC = 3, ICNN_CALL_CONV_MAXPOOL = 4, ICNN_CALL_BOTTLENECK = 5,
     ICNN_CALL_BOTTLENECK_DUAL = 6, ICNN_CALL_PAIR = 7, ICNN_CALL_TWIN = 8, ICNN_CALL_CHAIN = 9, ICNN_CALL_MAXPOOL = 10, ICNN_CALL_AVGPOOL = 11,
     ICNN_CALL_CONV_MAXPOOL_PC = 12, ICNN_CALL_BOTTLENECK_PC = 13, ICNN_CALL_BOTTLENECK_DUAL_PC = 14, ICNN_CALL_PAIR_PC = 15,
-    ICNN_CALL_TWIN_LAST = 16, ICNN_CALL_TRIPLE = 17, ICNN_CALL_TRIPLE_PC = 18
+    ICNN_CALL_TWIN_LAST = 16, ICNN_CALL_TRIPLE = 17, ICNN_CALL_TRIPLE_PC = 18,
+    ICNN_CALL_RMS_NORM = 19, ICNN_CALL_QUANTIZE_ROWS = 20, ICNN_CALL_LINEAR = 21, ICNN_CALL_GATED_LINEAR = 22
 } icnn_call_kind;
 typedef struct {
     int32_t kind;                  /* icnn_call_kind */
@@ -532,6 +537,83 @@ int iavgpool_global_u8(int32_t n, int32_t h, int32_t w, int32_t c, int32_t mul,
  * out[i] = x[i] - 128 stored as int8.  `count` elements; in place is allowed.
  * (iconv2d_brelu can do the same on the fly with in_sub128 = 1.) */
 int irenormalize_u8(int64_t count, const void *x, void *out, void *stream);
+
+/*
+ * The feed-forward half of a transformer block in 8 bits.  The weights' side is that of the integer layers (Section 3.1: 8-bit weights without a
+ * zero point, one step per output channel as in Section 3.4.3), and so are the sums (int32, exact).  The scales are real numbers found at run time, one
+ * per row of activations, because the stream between such blocks is floating point: a number q of a row with scale s stands for q * s.
+ *
+ *   irms_norm_s8        sum = x + residual; q, scale = rows of rms_norm(sum) * gamma in 8 bits
+ *   igated_linear_s8    hidden = act(q Wg) * (q Wu)
+ *   iquantize_rows_s8   q, scale = rows of hidden in 8 bits
+ *   ilinear_s8          stream = act(q W) + residual
+ *
+ * One row is one token; every count of rows from none (the call does nothing) upwards is taken, and every k, c and n.  Strides are in elements of the
+ * tensor they belong to, from row to row; rows may start at any multiple of the element's size.  Arithmetic is in float32, streams in 16 bits are rounded
+ * to nearest, ties to even, once where they are stored.  No pointer needs more than its element's alignment; 16-byte aligned tensors and rows
+ * (strides) take faster paths with the same results.
+ */
+typedef enum {
+    ICNN_ACT_NONE = 0,
+    ICNN_ACT_RELU = 1,
+    ICNN_ACT_SILU = 2,             /* v / (1 + exp(-v))                                                       */
+    ICNN_ACT_GELU = 3,             /* v * (1 + erf(v / sqrt 2)) / 2                                           */
+    ICNN_ACT_GELU_TANH = 4         /* v * (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2                     */
+} icnn_act;
+
+/*
+ * Rows of a stream to 8 bits.
+ *   s     = x + residual, rounded to the stream's type     (residual NULL: s = x)
+ *   sum   = s                                              (sum NULL: not stored; it may be x or the residual itself, with that one's stride)
+ *   u     = s / sqrt(mean over c of s^2 + eps) * gamma[c]  (iquantize_rows_s8: u = x)
+ *   scale = max over c of |u| / 127
+ *   q     = u / scale, to nearest, ties to even: in [-127, 127], the row's largest magnitude at 127
+ * A row of zeros (largest |s * gamma|, or |x|, below 2^-120) has scale 0 and numbers 0.  A row that holds a NaN or an infinity, or numbers
+ * whose squares or products with gamma leave float32, has scale NaN and numbers 0: each of its values is NaN.
+ * gamma: c numbers of gamma_dtype (the stream's type or ICNN_F32).  scale: `rows` float32.  No output may overlap an input (but for `sum` as above) or
+ * another output: ICNN_E_UNSUPPORTED.  iquantize_rows_s8 uses rows, c, x_stride, q_stride and dtype.
+ */
+typedef struct {
+    int64_t rows;                  /* 0 <= rows < 2^31                             */
+    int64_t x_stride, res_stride, sum_stride, q_stride;   /* c <= stride <= 2^40, rows * stride <= 2^44 */
+    int32_t c;                     /* 1 <= c <= 2^20                               */
+    int32_t dtype;                 /* of x, residual and sum: ICNN_F32, F16 or BF16 */
+    int32_t gamma_dtype;
+    float eps;                     /* >= 0, finite                                 */
+} icnn_norm_desc;
+
+int irms_norm_s8(const icnn_norm_desc *desc, const void *x, const void *residual, const void *gamma, void *sum, void *q, float *scale,
+                 void *stream);
+int iquantize_rows_s8(const icnn_norm_desc *desc, const void *x, void *q, float *scale, void *stream);
+
+/*
+ * Products of 8-bit rows.
+ *   v[m][n] = act(sum over k of x[m][k] * w[n][k] * x_scale[m] * w_scale[n] + bias[n])      (bias NULL: none)
+ *   ilinear_s8:        y = v + residual[m][n]                                              (residual NULL: none; it may be y itself)
+ *   igated_linear_s8:  y = v * (sum over k of x[m][k] * w_up[n][k] * x_scale[m] * up_scale[n] + up_bias[n]);   v of w_gate, gate_scale, gate_bias
+ * x: int8 [rows][k], w: int8 [n][k] as they are (no packing; both weights of a gated layer have w_stride), the sum over k in int32, exact
+ * for every k the descriptor allows and any bytes.  Scales and biases: float32, one per row or output.  y and residual: dtype.  y may not overlap
+ * another operand but its residual in place (same pointer and stride): ICNN_E_UNSUPPORTED.
+ * workspace: at least ..._workspace_bytes bytes, 16-byte aligned, zero-filled once by the caller after allocating it (its first 4096 bytes are
+ * counters that every call leaves at zero); NULL where that is 0.  One workspace of the largest size may serve all calls that run one after the
+ * other on a stream; calls that may overlap in time need one each.
+ */
+typedef struct {
+    int64_t rows;                  /* 0 <= rows < 2^31                             */
+    int64_t x_stride, w_stride;    /* >= k, and at most 2^40, rows (n) * stride at most 2^44 */
+    int64_t res_stride, y_stride;  /* >= n, likewise                               */
+    int32_t k, n;                  /* 1 <= k <= 131071 (the int32 sum is safe for any bytes), 1 <= n */
+    int32_t act;                   /* icnn_act                                     */
+    int32_t dtype;                 /* of y and residual: ICNN_F32, F16 or BF16     */
+} icnn_linear_desc;
+
+int ilinear_s8_workspace_bytes(const icnn_linear_desc *desc, size_t *bytes);
+int ilinear_s8(const icnn_linear_desc *desc, const void *x, const float *x_scale, const void *w, const float *w_scale, const float *bias,
+               const void *residual, void *y, void *workspace, void *stream);
+
+int igated_linear_s8_workspace_bytes(const icnn_linear_desc *desc, size_t *bytes);
+int igated_linear_s8(const icnn_linear_desc *desc, const void *x, const float *x_scale, const void *w_gate, const float *gate_scale,
+                     const float *gate_bias, const void *w_up, const float *up_scale, const float *up_bias, void *y, void *workspace, void *stream);
 
 /*
  * Measurement aids: the two roofs a convolution layer is judged against, as they are on the machine at hand

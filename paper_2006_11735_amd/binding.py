@@ -14,7 +14,8 @@ LIB_PATH = os.path.join(HERE, "libicnn_mi355.so")
 ICNN_OK = 0
 ICNN_IN_U8_LE127, ICNN_IN_S8, ICNN_IN_U8_FULL = 0, 1, 2
 ICNN_E_NULL, ICNN_E_SHAPE, ICNN_E_PARAM, ICNN_E_ALIGN, ICNN_E_UNSUPPORTED, ICNN_E_LAUNCH = -1, -2, -3, -4, -5, -6
-ICNN_U8, ICNN_S8, ICNN_S32 = 0, 1, 2
+ICNN_U8, ICNN_S8, ICNN_S32, ICNN_F32, ICNN_F16, ICNN_BF16 = range(6)
+ICNN_ACT_NONE, ICNN_ACT_RELU, ICNN_ACT_SILU, ICNN_ACT_GELU, ICNN_ACT_GELU_TANH = range(5)
 ICNN_OUT_BRELU_U8, ICNN_OUT_CLAMP_U8, ICNN_OUT_LINEAR_S8, ICNN_OUT_RAW_S32 = 0, 1, 2, 3
 ICNN_RES_NONE, ICNN_RES_PRE, ICNN_RES_POST = 0, 1, 2
 
@@ -37,6 +38,16 @@ class icnn_channel_params(C.Structure):
     _fields_ = [(k, C.c_void_p) for k in ("mul", "shift", "res_mul", "res_shift")]
 
 
+class icnn_norm_desc(C.Structure):
+    _fields_ = [(k, C.c_int64) for k in ("rows", "x_stride", "res_stride", "sum_stride", "q_stride")] + [
+        (k, C.c_int32) for k in ("c", "dtype", "gamma_dtype")] + [("eps", C.c_float)]
+
+
+class icnn_linear_desc(C.Structure):
+    _fields_ = [(k, C.c_int64) for k in ("rows", "x_stride", "w_stride", "res_stride", "y_stride")] + [
+        (k, C.c_int32) for k in ("k", "n", "act", "dtype")]
+
+
 class icnn_call(C.Structure):
     _fields_ = [("kind", C.c_int32), ("i", C.c_int32 * 7), ("d", C.POINTER(icnn_conv_desc) * 4), ("p", C.c_void_p * 13),
                 ("list", C.c_void_p * 3)]
@@ -44,7 +55,8 @@ class icnn_call(C.Structure):
 
 (ICNN_CALL_CONV, ICNN_CALL_CONV_PC, ICNN_CALL_DUAL, ICNN_CALL_DUAL_PC, ICNN_CALL_CONV_MAXPOOL, ICNN_CALL_BOTTLENECK, ICNN_CALL_BOTTLENECK_DUAL,
  ICNN_CALL_PAIR, ICNN_CALL_TWIN, ICNN_CALL_CHAIN, ICNN_CALL_MAXPOOL, ICNN_CALL_AVGPOOL, ICNN_CALL_CONV_MAXPOOL_PC, ICNN_CALL_BOTTLENECK_PC,
- ICNN_CALL_BOTTLENECK_DUAL_PC, ICNN_CALL_PAIR_PC, ICNN_CALL_TWIN_LAST, ICNN_CALL_TRIPLE, ICNN_CALL_TRIPLE_PC) = range(19)
+ ICNN_CALL_BOTTLENECK_DUAL_PC, ICNN_CALL_PAIR_PC, ICNN_CALL_TWIN_LAST, ICNN_CALL_TRIPLE, ICNN_CALL_TRIPLE_PC,
+ ICNN_CALL_RMS_NORM, ICNN_CALL_QUANTIZE_ROWS, ICNN_CALL_LINEAR, ICNN_CALL_GATED_LINEAR) = range(23)
 
 
 class IcnnError(RuntimeError):
@@ -103,6 +115,12 @@ _lib.iconcat.argtypes = [_i32, C.POINTER(_vp), C.POINTER(_i32), C.POINTER(_i32),
 _lib.imaxpool2d_u8.argtypes = [_i32] * 7 + [_vp, _vp, _vp]
 _lib.iavgpool_global_u8.argtypes = [_i32] * 7 + [_vp, _vp, _vp]
 _lib.irenormalize_u8.argtypes = [_i64, _vp, _vp, _vp]
+_normp, _linearp = C.POINTER(icnn_norm_desc), C.POINTER(icnn_linear_desc)
+_lib.irms_norm_s8.argtypes = [_normp] + [_vp] * 7
+_lib.iquantize_rows_s8.argtypes = [_normp] + [_vp] * 4
+_lib.ilinear_s8_workspace_bytes.argtypes = _lib.igated_linear_s8_workspace_bytes.argtypes = [_linearp, C.POINTER(C.c_size_t)]
+_lib.ilinear_s8.argtypes = [_linearp] + [_vp] * 9
+_lib.igated_linear_s8.argtypes = [_linearp] + [_vp] * 11
 _lib.icnn_peak_mfma_i8.argtypes = [_i32, _i32, _vp, _vp]
 _lib.icnn_peak_copy.argtypes = [_vp, _vp, C.c_size_t, _vp]
 
@@ -110,7 +128,8 @@ EXPORTS = ["icnn_version", "icnn_last_error", "icnn_set_tuning", "iconv2d_valida
            "iconv2d_workspace_bytes", "iconv2d_packed_weight_bytes", "iconv2d_prepack_weights",
            "iconv2d_brelu", "iconv2d_brelu_static_ws", "iconv2d_packed_channel_params_bytes", "iconv2d_prepack_channel_params", "iconv2d_brelu_pc",
            "iconv2d_dual_brelu", "iconv2d_dual_brelu_pc", "iconv2d_bottleneck_brelu", "iconv2d_bottleneck_dual_brelu", "iconv2d_pair_brelu", "iconv2d_maxpool_brelu_pc", "iconv2d_bottleneck_brelu_pc", "iconv2d_bottleneck_dual_brelu_pc", "iconv2d_pair_brelu_pc", "iconv2d_triple_brelu", "iconv2d_triple_brelu_pc", "iconv2d_twin_brelu", "iconv2d_twin_last_brelu", "iconv2d_maxpool_brelu", "iconv2d_chain_brelu", "iconv2d_chain_split", "icnn_run_calls", "icnn_lanes_create", "icnn_lanes_destroy", "icnn_run_lanes", "iadd_rescale", "iconcat", "imaxpool2d_u8", "iavgpool_global_u8",
-           "irenormalize_u8", "icnn_peak_mfma_i8", "icnn_peak_copy"]
+           "irenormalize_u8", "irms_norm_s8", "iquantize_rows_s8", "ilinear_s8_workspace_bytes", "ilinear_s8", "igated_linear_s8_workspace_bytes",
+           "igated_linear_s8", "icnn_peak_mfma_i8", "icnn_peak_copy"]
 
 
 def _ptr(t):
@@ -162,6 +181,33 @@ def conv_desc(**kw):
             raise AttributeError(k)
         setattr(d, k, int(v))
     return d
+
+
+def _strided(d, kw, widths):
+    """Fields from `kw`; a stride that is not given is its rows' width."""
+    for k, v in kw.items():
+        if not hasattr(d, k):
+            raise AttributeError(k)
+        setattr(d, k, float(v) if k == "eps" else int(v))
+    for k, width in widths.items():
+        if k not in kw:
+            setattr(d, k, getattr(d, width))
+    return d
+
+
+def norm_desc(**kw):
+    """Descriptor of irms_norm_s8 and iquantize_rows_s8: dense rows of bfloat16 with a gamma of their type, where not given otherwise."""
+    d = icnn_norm_desc()
+    d.dtype, d.eps = ICNN_BF16, 1e-5
+    d.gamma_dtype = kw.get("dtype", ICNN_BF16)
+    return _strided(d, kw, {"x_stride": "c", "res_stride": "c", "sum_stride": "c", "q_stride": "c"})
+
+
+def linear_desc(**kw):
+    """Descriptor of ilinear_s8 and igated_linear_s8: dense rows, no activation, bfloat16 results, where not given otherwise."""
+    d = icnn_linear_desc()
+    d.dtype = ICNN_BF16
+    return _strided(d, kw, {"x_stride": "k", "w_stride": "k", "res_stride": "n", "y_stride": "n"})
 
 
 def add_desc(**kw):
@@ -337,6 +383,9 @@ def iconv2d_chain_split(descs):
     return list(lens[:k.value])
 
 
+FEED_FORWARD = {"rms_norm": ICNN_CALL_RMS_NORM, "quantize_rows": ICNN_CALL_QUANTIZE_ROWS, "linear": ICNN_CALL_LINEAR, "gated_linear": ICNN_CALL_GATED_LINEAR}
+
+
 class Calls:
     """A list of calls issued by one icnn_run_calls: (kind name, arguments of the binding's function of that kind), as netrun has them."""
 
@@ -358,6 +407,13 @@ class Calls:
             c.kind, c.i[0] = ICNN_CALL_CHAIN, n
             c.list[0], c.list[1], c.list[2] = C.addressof(dp), C.addressof(wp), C.addressof(bp)
             c.p[0], c.p[1] = _ptr(x), _ptr(y)
+            return
+        if kind in FEED_FORWARD:
+            d, *ptrs = args
+            c.kind = FEED_FORWARD[kind]
+            c.list[0] = C.addressof(d)
+            for k, t in enumerate(ptrs):
+                c.p[k] = _ptr(t)
             return
         if kind in ("triple", "triple_pc"):
             args = list(args)
@@ -442,6 +498,36 @@ def iavgpool_global_u8(n, h, w, c, mul, shift, bound_q, x, out, stream=None):
 
 def irenormalize_u8(count, x, out, stream=None):
     return _check(_lib.irenormalize_u8(count, _ptr(x), _ptr(out), _stream(stream)))
+
+
+def irms_norm_s8(desc, x, residual, gamma, sum, q, scale, stream=None):
+    return _check(_lib.irms_norm_s8(C.byref(desc), _ptr(x), _ptr(residual), _ptr(gamma), _ptr(sum), _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def iquantize_rows_s8(desc, x, q, scale, stream=None):
+    return _check(_lib.iquantize_rows_s8(C.byref(desc), _ptr(x), _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def ilinear_s8_workspace_bytes(desc):
+    size = C.c_size_t()
+    _check(_lib.ilinear_s8_workspace_bytes(C.byref(desc), C.byref(size)))
+    return size.value
+
+
+def ilinear_s8(desc, x, x_scale, w, w_scale, bias, residual, y, workspace=None, stream=None):
+    return _check(_lib.ilinear_s8(C.byref(desc), _ptr(x), _ptr(x_scale), _ptr(w), _ptr(w_scale), _ptr(bias), _ptr(residual), _ptr(y),
+                                  _ptr(workspace), _stream(stream)))
+
+
+def igated_linear_s8_workspace_bytes(desc):
+    size = C.c_size_t()
+    _check(_lib.igated_linear_s8_workspace_bytes(C.byref(desc), C.byref(size)))
+    return size.value
+
+
+def igated_linear_s8(desc, x, x_scale, w_gate, gate_scale, gate_bias, w_up, up_scale, up_bias, y, workspace=None, stream=None):
+    return _check(_lib.igated_linear_s8(C.byref(desc), _ptr(x), _ptr(x_scale), _ptr(w_gate), _ptr(gate_scale), _ptr(gate_bias), _ptr(w_up),
+                                        _ptr(up_scale), _ptr(up_bias), _ptr(y), _ptr(workspace), _stream(stream)))
 
 
 def icnn_peak_mfma_i8(blocks, iters, sink, stream=None):

@@ -12,11 +12,8 @@ using namespace icnn;
 
 namespace icnn {
 Tuning g_tuning;
-}
 
-namespace {
-
-thread_local char g_err[256] = "";
+static thread_local char g_err[256] = "";
 
 int fail(int code, const char *fmt, ...)
 {
@@ -26,6 +23,9 @@ int fail(int code, const char *fmt, ...)
     va_end(ap);
     return code;
 }
+}  // namespace icnn
+
+namespace {
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
@@ -1239,6 +1239,7 @@ static int run_call(int32_t k, const icnn_call &c, void *stream)
     const int32_t *i = c.i;
     auto b = [&](int q) { return (const int32_t *)p[q]; };
     auto o = [&](int q) { return const_cast<void *>(p[q]); };
+    auto f = [&](int q) { return (float *)const_cast<void *>(p[q]); };
     int rc;
     switch (c.kind) {
     case ICNN_CALL_CONV: rc = iconv2d_brelu(d[0], p[0], p[1], b(2), p[3], o(4), o(5), stream); break;
@@ -1260,6 +1261,14 @@ static int run_call(int32_t k, const icnn_call &c, void *stream)
     case ICNN_CALL_CHAIN:
         rc = iconv2d_chain_brelu(i[0], (const icnn_conv_desc *const *)c.list[0], p[0], (const void *const *)c.list[1],
                                  (const int32_t *const *)c.list[2], o(1), stream);
+        break;
+    case ICNN_CALL_RMS_NORM: rc = irms_norm_s8((const icnn_norm_desc *)c.list[0], p[0], p[1], p[2], o(3), o(4), f(5), stream); break;
+    case ICNN_CALL_QUANTIZE_ROWS: rc = iquantize_rows_s8((const icnn_norm_desc *)c.list[0], p[0], o(1), f(2), stream); break;
+    case ICNN_CALL_LINEAR:
+        rc = ilinear_s8((const icnn_linear_desc *)c.list[0], p[0], f(1), p[2], f(3), f(4), p[5], o(6), o(7), stream);
+        break;
+    case ICNN_CALL_GATED_LINEAR:
+        rc = igated_linear_s8((const icnn_linear_desc *)c.list[0], p[0], f(1), p[2], f(3), f(4), p[5], f(6), f(7), o(8), o(9), stream);
         break;
     case ICNN_CALL_CONV_MAXPOOL_PC: rc = iconv2d_maxpool_brelu_pc(d[0], i[0], i[1], i[2], p[0], p[1], b(2), p[3], o(4), stream); break;
     case ICNN_CALL_BOTTLENECK_PC:

@@ -1,0 +1,90 @@
+// Products of 8-bit rows and 8-bit weights with a scale per row and one per output:
+//   acc = sum_k x[m][k] w[n][k] (int32, exact: k <= 131071), v = acc * xs[m] * ws[n] + bias[n],
+//   y[m][n] = act(v) + res[m][n], or, gated, act(v) * v2 with v2 of the second weights; rounded to the stream's type once.
+// Weights are read as they are stored, [n][k] rows: both operands of the matrix instruction run along k, and the order of k is free as long as both sides
+// have the same.
+#include "ffn_common.h"
+
+namespace icnn {
+
+typedef int v4i_any __attribute__((ext_vector_type(4), aligned(1)));
+
+// 16 numbers k0.. of a row of K, zeros behind its end; reads no byte outside the row
+__device__ __forceinline__ v4i load_k16(const int8_t *row, int k0, int K)
+{
+    if (k0 + 16 <= K) return *(const v4i_any *)(row + k0);
+    v4i r = {};
+#pragma unroll
+    for (int b = 0; b < 16; ++b)
+        if (k0 + b < K) r[b >> 2] |= (int)(uint8_t)row[k0 + b] << (8 * (b & 3));
+    return r;
+}
+
+// Wait states between the last products and their sums' first reader (see mfma_drain in conv_common.h)
+template <int N>
+__device__ __forceinline__ void drain(v4i (&acc)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(acc[i]));
+    asm volatile("s_nop 15\n\ts_nop 3");
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(acc[i]));
+}
+
+// One output: y[m][n] from the sums of one product, or two
+template <bool GATED>
+__device__ __forceinline__ float finish(const LinearArgs &a, int acc, int acc2, float xs, int n)
+{
+    float v = (float)acc * xs * a.ws[n];
+    if (a.bias) v += a.bias[n];
+    v = activate(v, a.act);
+    if (GATED) {
+        float v2 = (float)acc2 * xs * a.ws2[n];
+        if (a.bias2) v2 += a.bias2[n];
+        v *= v2;
+    }
+    return v;
+}
+
+// One wave a tile of 16 x 16 outputs, operands straight from memory.
+template <bool GATED>
+__global__ __launch_bounds__(256) void linear_plain_kernel(const LinearArgs a, int tiles_n, long long tiles)
+{
+    const long long tile = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (tile >= tiles) return;
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int m0 = (int)(tile / tiles_n) * 16, n0 = (int)(tile % tiles_n) * 16;
+    const int8_t *const x = a.x + min(m0 + r, a.M - 1) * a.ldx;
+    const int8_t *const w = a.w + min(n0 + r, a.N - 1) * a.ldw;
+    const int8_t *const w2 = GATED ? a.w2 + min(n0 + r, a.N - 1) * a.ldw : nullptr;
+    v4i acc[2] = {};
+    for (int k = 16 * g; k - 16 * g < a.K; k += 64) {
+        const v4i xv = load_k16(x, k, a.K);
+        acc[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(load_k16(w, k, a.K), xv, acc[0], 0, 0, 0);
+        if (GATED) acc[1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(load_k16(w2, k, a.K), xv, acc[1], 0, 0, 0);
+    }
+    drain(acc);
+    const int m = m0 + r;
+    if (m >= a.M) return;
+    const float xs = a.xs[m];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int n = n0 + 4 * g + i;
+        if (n >= a.N) break;
+        float v = finish<GATED>(a, acc[0][i], acc[1][i], xs, n);
+        if (!GATED && a.res) v += load_number(a.res, m * a.ldr + n, a.dtype);
+        store_number(a.y, m * a.ldy + n, a.dtype, v);
+    }
+}
+
+hipError_t launch_linear(const LinearArgs &a, hipStream_t st)
+{
+    const int tiles_n = (a.N + 15) / 16;
+    const long long tiles = (long long)((a.M + 15) / 16) * tiles_n, blocks = (tiles + 3) / 4;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (a.w2) hipLaunchKernelGGL(linear_plain_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, a, tiles_n, tiles);
+    else hipLaunchKernelGGL(linear_plain_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, a, tiles_n, tiles);
+    return hipGetLastError();
+}
+
+}  // namespace icnn

@@ -1,0 +1,205 @@
+"""ilinear_s8 and igated_linear_s8 on the GPU against their definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from ff_util import ACTS, DTYPES, Placed, gated64, linear64, to_numpy
+from paper_2006_11735_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def weights(g, n, k, full):
+    w = g.integers(-128, 128, size=(n, k)) if full else np.clip(np.rint(g.normal(size=(n, k)) * 40), -127, 127)
+    return w.astype(np.int8), g.uniform(0.5, 1.5, size=n).astype(np.float32) / (40 * k ** 0.5)
+
+
+def run(rows, k, n, dtype="bf16", act="none", *, gated=False, bias=True, residual=False, in_place=False, pads=(0, 0, 0, 0), offset=0, seed=0, full=False,
+        stream=None, x=None):
+    """pads: of the rows of x, w, residual and y; offset: elements in front of every tensor"""
+    g = np.random.default_rng(seed)
+    torch_dtype, code = DTYPES[dtype]
+    xv = (np.clip(np.rint(g.normal(size=(rows, k)) * 40), -127, 127) if not full else g.integers(-128, 128, size=(rows, k))).astype(np.int8)
+    if x is not None:
+        xv = x
+    xs = g.uniform(0.5, 1.5, size=rows).astype(np.float32) / 40
+    layers = [weights(g, n, k, full) for _ in range(2 if gated else 1)]
+    biases = [g.normal(size=n).astype(np.float32) if bias else None for _ in layers]
+    rv = torch.from_numpy(g.normal(size=(rows, n))).to(torch_dtype) if residual else None
+
+    def vector(v):
+        return None if v is None else Placed(1, len(v), torch.float32, len(v), offset, torch.from_numpy(v))
+    X = Placed(rows, k, torch.int8, k + pads[0], offset, torch.from_numpy(xv))
+    W = [Placed(n, k, torch.int8, k + pads[1], offset, torch.from_numpy(w)) for w, _ in layers]
+    R = Placed(rows, n, torch_dtype, n + pads[2], offset, rv) if residual else None
+    Y = R if in_place else Placed(rows, n, torch_dtype, n + pads[3], offset)
+    scales, b, XS = [vector(s) for _, s in layers], [vector(v) for v in biases], vector(xs)
+    d = B.linear_desc(rows=rows, k=k, n=n, x_stride=X.stride, w_stride=W[0].stride, res_stride=R.stride if residual else n, y_stride=Y.stride,
+                      act=ACTS.index(act), dtype=code)
+    tensors = [t for t in [X, XS, R, Y, *W, *scales, *b] if t is not None]
+    for t in tensors:
+        t.snapshot()
+    size = (B.igated_linear_s8_workspace_bytes if gated else B.ilinear_s8_workspace_bytes)(d)
+    ws = torch.zeros(size, dtype=torch.uint8, device="cuda:0") if size else None
+    torch.cuda.synchronize()
+    for _ in range(2 if ws is not None and not in_place else 1):          # (the second call finds the workspace as the first has left it)
+        if gated:
+            B.igated_linear_s8(d, X, XS, W[0], scales[0], b[0], W[1], scales[1], b[1], Y, ws, stream=stream)
+        else:
+            B.ilinear_s8(d, X, XS, W[0], scales[0], b[0], R, Y, ws, stream=stream)
+    torch.cuda.synchronize()
+    assert all(t.rest_untouched() for t in tensors)
+    assert all((t.raw == t.before).all() for t in tensors if t is not Y)
+    if ws is not None:
+        assert not ws[:4096].any()
+    if gated:
+        want, tol = gated64(xv, xs, layers[0][0], layers[0][1], biases[0], layers[1][0], layers[1][1], biases[1], act, dtype)
+    else:
+        want, tol = linear64(xv, xs, layers[0][0], layers[0][1], biases[0], act, None if rv is None else to_numpy(rv), dtype)
+    got = to_numpy(Y.view)
+    assert got.shape == want.shape
+    off = np.abs(got - want) - tol
+    assert (off <= 0).all(), (float(off.max()), np.unravel_index(np.argmax(off), off.shape))
+    return got
+
+
+ROWS = [1, 2, 3, 7, 15, 16, 17, 31, 32, 33, 48, 64, 65, 100, 128, 129, 200, 257]
+
+
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("k,n", [(256, 192), (1000, 100), (129, 65)])
+def test_row_counts(rows, gated, k, n):
+    run(rows, k, n, "f32", "silu" if gated else "none", gated=gated, residual=not gated, seed=rows)
+
+
+@pytest.mark.parametrize("k", [1, 2, 15, 16, 17, 31, 48, 63, 64, 65, 80, 127, 128, 130, 144, 255, 256, 272, 511, 1001, 2048, 5000])
+@pytest.mark.parametrize("rows,n", [(1, 33), (40, 70), (130, 140)])
+def test_depths(k, rows, n):
+    run(rows, k, n, "f32", seed=k)
+    run(rows, k, n, "f32", "silu", gated=True, seed=k)
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 8, 15, 16, 17, 31, 33, 64, 127, 128, 129, 255, 257, 1000])
+@pytest.mark.parametrize("rows,k", [(1, 512), (20, 256), (90, 256), (260, 128)])
+def test_widths(n, rows, k):
+    run(rows, k, n, "f16", residual=True, seed=n)
+    run(rows, k, n, "f16", "gelu_tanh", gated=True, seed=n)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("rows", [1, 37, 300])
+def test_types_and_activations(dtype, act, rows):
+    run(rows, 384, 272, dtype, act, residual=True, seed=1)
+    run(rows, 384, 272, dtype, act, bias=False, seed=2)
+    run(rows, 384, 272, dtype, act, gated=True, seed=3)
+    run(rows, 384, 272, dtype, act, gated=True, bias=False, seed=4)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("pads,offset", [((16, 32, 8, 24), 0), ((16, 16, 16, 16), 16), ((0, 0, 0, 0), 1), ((1, 3, 5, 7), 5), ((16, 0, 1, 0), 0), ((0, 16, 0, 3), 0),
+                                         ((8, 8, 8, 8), 8), ((4, 4, 4, 4), 4)])
+@pytest.mark.parametrize("rows,k,n", [(1, 320, 144), (29, 320, 144), (140, 640, 272), (140, 333, 111)])
+def test_strides_and_offsets(dtype, pads, offset, rows, k, n):
+    run(rows, k, n, dtype, "gelu", residual=True, pads=pads, offset=offset, seed=7)
+    run(rows, k, n, dtype, "silu", gated=True, pads=pads, offset=offset, seed=8)
+
+
+@pytest.mark.parametrize("rows", [1, 20, 150])
+def test_residual_in_place(rows):
+    run(rows, 512, 256, "bf16", "none", residual=True, in_place=True, pads=(0, 0, 16, 16))
+
+
+@pytest.mark.parametrize("rows,k,n,gated", [(1, 16384, 512, False), (3, 8192, 1024, True), (16, 12288, 96, False), (64, 16384, 128, False), (300, 8192, 256, True),
+                                            (512, 1024, 2048, False), (777, 512, 1111, True), (1024, 2048, 1024, False), (1300, 640, 1536, True)])
+def test_larger_products(rows, k, n, gated):
+    run(rows, k, n, "bf16", "silu" if gated else "none", gated=gated, residual=not gated, seed=5)
+
+
+def test_the_deepest_sum_of_the_largest_numbers():
+    """k = 131071 with every product 128 * 128: the sum is 2^31 - 16384"""
+    k, rows, n = 131071, 3, 5
+    d = B.linear_desc(rows=rows, k=k, n=n, dtype=B.ICNN_F32)
+    x = torch.full((rows, k), -128, dtype=torch.int8, device="cuda:0")
+    w = torch.full((n, k), -128, dtype=torch.int8, device="cuda:0")
+    one = torch.ones(8, device="cuda:0")
+    y = torch.zeros((rows, n), device="cuda:0")
+    size = B.ilinear_s8_workspace_bytes(d)
+    ws = torch.zeros(size, dtype=torch.uint8, device="cuda:0") if size else None
+    B.ilinear_s8(d, x, one, w, one, None, None, y, ws)
+    torch.cuda.synchronize()
+    assert (y == float(np.float32(k * 16384))).all()
+
+
+@pytest.mark.parametrize("rows", [1, 40, 200])
+def test_any_bytes(rows):
+    run(rows, 700, 90, "f32", full=True, seed=11)
+    run(rows, 704, 96, "f32", "relu", gated=True, full=True, seed=12)
+
+
+def test_rows_of_zeros_and_scales_that_are_nan():
+    x = np.zeros((4, 128), np.int8)
+    run(4, 128, 64, "bf16", "silu", gated=True, x=x)
+    d = B.linear_desc(rows=2, k=128, n=64)
+    xs = torch.tensor([float("nan"), 1.0], device="cuda:0")
+    w = torch.ones((64, 128), dtype=torch.int8, device="cuda:0")
+    ws = torch.ones(64, device="cuda:0")
+    y = torch.zeros((2, 64), dtype=torch.bfloat16, device="cuda:0")
+    B.ilinear_s8(d, torch.zeros((2, 128), dtype=torch.int8, device="cuda:0"), xs, w, ws, None, None, y)
+    torch.cuda.synchronize()
+    assert y[0].isnan().all() and (y[1] == 0).all()
+
+
+def test_no_rows_is_a_call_that_does_nothing():
+    d = B.linear_desc(rows=0, k=64, n=32)
+    assert B.ilinear_s8_workspace_bytes(d) == 0 and B.igated_linear_s8_workspace_bytes(d) == 0
+    B.ilinear_s8(d, None, None, None, None, None, None, None)
+    B.igated_linear_s8(d, None, None, None, None, None, None, None, None, None)
+
+
+@pytest.mark.parametrize("rows", [3, 70, 300])
+def test_rows_beyond_32_bits(rows):
+    """The last rows of x and y lie more than 2^32 bytes behind the first."""
+    k, n, stride = 256, 128, ((1 << 32) // (rows - 1) + 4096) // 4096 * 4096
+    g = np.random.default_rng(3)
+    x = torch.empty((rows - 1) * stride + k, dtype=torch.int8, device="cuda:0")
+    y = torch.empty((rows - 1) * stride + n, dtype=torch.float16, device="cuda:0")
+    xv, (wv, ws) = g.integers(-127, 128, size=(rows, k)).astype(np.int8), weights(g, n, k, False)
+    xs = g.uniform(0.5, 1.5, size=rows).astype(np.float32) / 40
+    x.as_strided((rows, k), (stride, 1)).copy_(torch.from_numpy(xv))
+    dev = lambda v: torch.from_numpy(v).to("cuda:0")  # noqa: E731
+    d = B.linear_desc(rows=rows, k=k, n=n, x_stride=stride, y_stride=stride, res_stride=stride, dtype=B.ICNN_F16)
+    size = B.ilinear_s8_workspace_bytes(d)
+    space = torch.zeros(size, dtype=torch.uint8, device="cuda:0") if size else None
+    W, WS, XS = dev(wv), dev(ws), dev(xs)
+    B.ilinear_s8(d, x, XS, W, WS, None, None, y, space)
+    torch.cuda.synchronize()
+    want, tol = linear64(xv, xs, wv, ws, None, "none", None, "f16")
+    assert (np.abs(to_numpy(y.as_strided((rows, n), (stride, 1))) - want) <= tol).all()
+
+
+def test_weights_beyond_32_bits():
+    k, n = 128, 40
+    stride = ((1 << 32) // (n - 1) + 4096) // 4096 * 4096
+    g = np.random.default_rng(4)
+    w = torch.empty((n - 1) * stride + k, dtype=torch.int8, device="cuda:0")
+    wv, ws = weights(g, n, k, False)
+    w.as_strided((n, k), (stride, 1)).copy_(torch.from_numpy(wv))
+    WS = torch.from_numpy(ws).to("cuda:0")
+    for rows in (2, 100):
+        xv, xs = g.integers(-127, 128, size=(rows, k)).astype(np.int8), g.uniform(0.5, 1.5, size=rows).astype(np.float32) / 40
+        X, XS = torch.from_numpy(xv).to("cuda:0"), torch.from_numpy(xs).to("cuda:0")
+        y = torch.empty((rows, n), dtype=torch.float32, device="cuda:0")
+        d = B.linear_desc(rows=rows, k=k, n=n, w_stride=stride, dtype=B.ICNN_F32)
+        size = B.ilinear_s8_workspace_bytes(d)
+        B.ilinear_s8(d, X, XS, w, WS, None, None, y, torch.zeros(size, dtype=torch.uint8, device="cuda:0") if size else None)
+        torch.cuda.synchronize()
+        want, tol = linear64(xv, xs, wv, ws, None, "none", None, "f32")
+        assert (np.abs(to_numpy(y) - want) <= tol).all()
+
+
+def test_on_a_stream_of_its_own():
+    st = torch.cuda.Stream()
+    run(33, 512, 320, "bf16", "silu", gated=True, stream=st)
+    run(400, 512, 320, "bf16", residual=True, stream=st)

@@ -1,0 +1,170 @@
+"""irms_norm_s8 and iquantize_rows_s8 on the GPU against their definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from ff_util import DTYPES, Placed, rows64, to_numpy
+from paper_2006_11735_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def check(q, scale, s, gamma, eps):
+    """s: the stored sums.  The scale is a mean of c squares in float32 (at most c / 64 + 16 roundings in a row, halved by the root), and five roundings.
+    A number is off the exact quotient by the products with gamma and the factor and the factor's own three roundings: 5 of 2^-24 of at most 127."""
+    u, want = rows64(s, gamma, eps)
+    c = s.shape[1]
+    tol = (c / 64 + 16) * 2.0 ** -25 + 5 * 2.0 ** -24
+    assert (np.abs(scale - want) <= tol * want).all()
+    live = want > 0
+    exact = u[live] / want[live][:, None]
+    assert (np.abs(q[live] - exact) <= 0.5 + 127 * 5 * 2.0 ** -24).all()
+    assert (np.abs(q[live]).max(1) == 127).all()
+    assert (q[~live] == 0).all() and (scale[~live] == 0).all()
+
+
+def run_norm(rows, c, dtype, *, residual=True, keep=True, gamma_f32=False, pads=(0, 0, 0, 0), offset=0, alias=None, seed=0, x=None, stream=None):
+    """alias: "x" or "res" = the sum goes over that tensor"""
+    torch_dtype, code = DTYPES[dtype]
+    g = torch.Generator().manual_seed(seed)
+    xv = torch.randn((rows, c), generator=g).to(torch_dtype) if x is None else x.to(torch_dtype)
+    rv = torch.randn((rows, c), generator=g).to(torch_dtype)
+    gv = (torch.rand(c, generator=g) + 0.5).to(torch.float32 if gamma_f32 else torch_dtype)
+    X, R = Placed(rows, c, torch_dtype, c + pads[0], offset, xv), Placed(rows, c, torch_dtype, c + pads[1], offset, rv)
+    S = {"x": X, "res": R}.get(alias) or Placed(rows, c, torch_dtype, c + pads[2], offset)
+    Q, G, scale = Placed(rows, c, torch.int8, c + pads[3], offset), Placed(1, c, gv.dtype, c, offset, gv), Placed(1, rows, torch.float32, rows, offset)
+    d = B.norm_desc(rows=rows, c=c, x_stride=X.stride, res_stride=R.stride, sum_stride=S.stride, q_stride=Q.stride, dtype=code,
+                    gamma_dtype=B.ICNN_F32 if gamma_f32 else code, eps=1e-5)
+    tensors = [X, R, S, Q, G, scale]
+    for t in tensors:
+        t.snapshot()
+    torch.cuda.synchronize()
+    B.irms_norm_s8(d, X, R if residual else None, G, S if keep else None, Q, scale, stream=stream)
+    torch.cuda.synchronize()
+    assert all(t.rest_untouched() for t in tensors)
+    want_sum = (xv.float() + rv.float()).to(torch_dtype) if residual else xv
+    if keep:
+        same = (S.view.cpu() == want_sum) | (S.view.cpu().isnan() & want_sum.isnan())
+        assert same.all()
+    else:
+        assert (S.raw == S.before).all()
+    if alias is None:
+        assert (X.raw == X.before).all() and (R.raw == R.before).all()
+    return to_numpy(Q.view).astype(np.int64), to_numpy(scale.view)[0], to_numpy(want_sum), to_numpy(gv)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("c", [1, 7, 64, 255, 1000, 1024, 2049, 4096, 8192, 8200, 12288, 16384, 16391, 40000])
+def test_norm_of_widths(dtype, c):
+    q, scale, s, gamma = run_norm(5, c, dtype, seed=c)
+    check(q, scale, s, gamma, 1e-5)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 63, 300, 1025])
+@pytest.mark.parametrize("c", [128, 333, 2048])
+def test_norm_of_row_counts(rows, c):
+    q, scale, s, gamma = run_norm(rows, c, "bf16", seed=rows)
+    check(q, scale, s, gamma, 1e-5)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("pads,offset", [((8, 16, 24, 32), 0), ((0, 0, 0, 0), 1), ((1, 3, 5, 7), 3), ((8, 8, 8, 5), 8), ((3, 8, 8, 16), 16)])
+@pytest.mark.parametrize("c", [96, 1536, 9000])
+def test_norm_with_strides_and_offsets(dtype, pads, offset, c):
+    q, scale, s, gamma = run_norm(6, c, dtype, pads=pads, offset=offset, seed=offset)
+    check(q, scale, s, gamma, 1e-5)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("residual,keep,gamma_f32,alias", [(False, False, False, None), (False, True, True, None), (True, False, False, None),
+                                                            (True, True, True, "x"), (True, True, False, "res"), (False, True, False, "x")])
+@pytest.mark.parametrize("c", [130, 4096, 20000])
+def test_norm_with_and_without_its_parts(dtype, residual, keep, gamma_f32, alias, c):
+    q, scale, s, gamma = run_norm(9, c, dtype, residual=residual, keep=keep, gamma_f32=gamma_f32, alias=alias, seed=3)
+    check(q, scale, s, gamma, 1e-5)
+
+
+@pytest.mark.parametrize("c", [64, 1000, 4096, 17000])
+def test_rows_of_zeros_nan_and_infinity(c):
+    x = torch.randn((6, c), generator=torch.Generator().manual_seed(1))
+    x[1] = 0
+    x[2, c // 2] = float("nan")
+    x[3, c - 1] = float("inf")
+    x[4, 0] = float("-inf")
+    for dtype in DTYPES:
+        q, scale, s, gamma = run_norm(6, c, dtype, residual=False, x=x)
+        for k in (2, 3, 4):
+            assert np.isnan(scale[k]) and (q[k] == 0).all()
+        keep = [0, 1, 5]
+        check(q[keep], scale[keep], s[keep], gamma, 1e-5)
+        assert scale[1] == 0
+        q, scale, s = run_quantize(6, c, dtype, x=x)
+        for k in (2, 3, 4):
+            assert np.isnan(scale[k]) and (q[k] == 0).all()
+        check(q[keep], scale[keep], s[keep], None, 0)
+
+
+def test_one_large_number_among_small_ones_and_the_range_of_f16():
+    x = torch.full((3, 4096), 1e-3)
+    x[0, 17] = 6e4                       # near the largest of float16
+    x[1] = 6e-8                          # its least one
+    x[2, ::2] = -1e-3
+    for dtype in DTYPES:
+        q, scale, s, gamma = run_norm(3, 4096, dtype, residual=False, x=x)
+        check(q, scale, s, gamma, 1e-5)
+        q, scale, s = run_quantize(3, 4096, dtype, x=x)
+        check(q, scale, s, None, 0)
+
+
+def run_quantize(rows, c, dtype, pad=0, offset=0, x=None, seed=0):
+    torch_dtype, code = DTYPES[dtype]
+    xv = (torch.randn((rows, c), generator=torch.Generator().manual_seed(seed)) if x is None else x).to(torch_dtype)
+    X, Q, scale = Placed(rows, c, torch_dtype, c + pad, offset, xv), Placed(rows, c, torch.int8, c + pad, offset), Placed(1, rows, torch.float32, rows)
+    tensors = [X, Q, scale]
+    for t in tensors:
+        t.snapshot()
+    B.iquantize_rows_s8(B.norm_desc(rows=rows, c=c, x_stride=X.stride, q_stride=Q.stride, dtype=code), X, Q, scale)
+    torch.cuda.synchronize()
+    assert all(t.rest_untouched() for t in tensors) and (X.raw == X.before).all()
+    return to_numpy(Q.view).astype(np.int64), to_numpy(scale.view)[0], to_numpy(xv)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,c,pad,offset", [(1, 1, 0, 0), (1, 16384, 0, 0), (3, 16385, 0, 0), (70, 512, 0, 0), (70, 513, 0, 0), (33, 4096, 16, 0), (5, 100, 3, 1),
+                                               (2, 70000, 0, 0)])
+def test_rows_without_a_norm(dtype, rows, c, pad, offset):
+    q, scale, s = run_quantize(rows, c, dtype, pad, offset)
+    check(q, scale, s, None, 0)
+
+
+def test_ties_go_to_even():
+    x = torch.tensor([[127.0, 0.5, 1.5, 2.5, -0.5, -1.5, -2.5, 126.5]])
+    q, scale, _ = run_quantize(1, 8, "f32", x=x)
+    assert q[0].tolist() == [127, 0, 2, 2, 0, -2, -2, 126] and scale[0] == 1
+
+
+def test_no_rows_is_a_call_that_does_nothing():
+    d = B.norm_desc(rows=0, c=64)
+    B.irms_norm_s8(d, None, None, None, None, None, None)
+    B.iquantize_rows_s8(d, None, None, None)
+
+
+def test_rows_beyond_32_bits():
+    # the last row lies more than 2^32 elements behind the first
+    stride = (1 << 31) + 8
+    x = torch.empty(2 * stride + 512, dtype=torch.bfloat16, device="cuda:0")
+    q = torch.empty(2 * stride + 512, dtype=torch.int8, device="cuda:0")
+    v = torch.randn((3, 512), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16)
+    x.as_strided((3, 512), (stride, 1)).copy_(v)
+    scale = torch.empty(3, device="cuda:0")
+    gamma = torch.ones(512, dtype=torch.bfloat16, device="cuda:0")
+    d = B.norm_desc(rows=3, c=512, x_stride=stride, sum_stride=stride, q_stride=stride)
+    B.irms_norm_s8(d, x, None, gamma, x, q, scale)
+    torch.cuda.synchronize()
+    check(to_numpy(q.as_strided((3, 512), (stride, 1))).astype(np.int64), to_numpy(scale), to_numpy(v), np.ones(512), 1e-5)
+
+
+def test_on_a_stream_of_its_own():
+    st = torch.cuda.Stream()
+    q, scale, s, gamma = run_norm(40, 2048, "f16", stream=st)
+    check(q, scale, s, gamma, 1e-5)
