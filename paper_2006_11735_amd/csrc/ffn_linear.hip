@@ -7,8 +7,6 @@
 
 namespace icnn {
 
-typedef int v4i_any __attribute__((ext_vector_type(4), aligned(1)));
-
 // 16 numbers k0.. of a row of K, zeros behind its end; reads no byte outside the row
 __device__ __forceinline__ v4i load_k16(const int8_t *row, int k0, int K)
 {
@@ -79,6 +77,7 @@ __global__ __launch_bounds__(256) void linear_plain_kernel(const LinearArgs a, i
 
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st)
 {
+    if (tiled_linear_takes(a)) return launch_tiled_linear(a, st);
     const int tiles_n = (a.N + 15) / 16;
     const long long tiles = (long long)((a.M + 15) / 16) * tiles_n, blocks = (tiles + 3) / 4;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
