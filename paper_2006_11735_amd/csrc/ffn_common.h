@@ -30,6 +30,8 @@ struct LinearArgs {
 
 hipError_t launch_rows(const RowsArgs &a, hipStream_t st);
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st);
+bool few_linear_takes(const LinearArgs &a);
+hipError_t launch_few_linear(const LinearArgs &a, hipStream_t st);
 bool tiled_linear_takes(const LinearArgs &a);
 hipError_t launch_tiled_linear(const LinearArgs &a, hipStream_t st);
 
@@ -67,6 +69,32 @@ __device__ __forceinline__ float activate(float v, int act)
     if (act == 2) return v * logistic(v);
     if (act == 3) return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
     if (act == 4) return v * logistic(1.5957691216057308f * (v + 0.044715f * v * v * v));
+    return v;
+}
+
+// 16 numbers k0.. of a row of K, zeros behind its end; reads no byte outside the row
+__device__ __forceinline__ v4i load_k16(const int8_t *row, int k0, int K)
+{
+    if (k0 + 16 <= K) return *(const v4i_any *)(row + k0);
+    v4i r = {};
+#pragma unroll
+    for (int b = 0; b < 16; ++b)
+        if (k0 + b < K) r[b >> 2] |= (int)(uint8_t)row[k0 + b] << (8 * (b & 3));
+    return r;
+}
+
+// One output: y[m][n] from the sums of one product, or two
+template <bool GATED>
+__device__ __forceinline__ float finish(const LinearArgs &a, int acc, int acc2, float xs, int n)
+{
+    float v = (float)acc * xs * a.ws[n];
+    if (a.bias) v += a.bias[n];
+    v = activate(v, a.act);
+    if (GATED) {
+        float v2 = (float)acc2 * xs * a.ws2[n];
+        if (a.bias2) v2 += a.bias2[n];
+        v *= v2;
+    }
     return v;
 }
 

@@ -7,17 +7,6 @@
 
 namespace icnn {
 
-// 16 numbers k0.. of a row of K, zeros behind its end; reads no byte outside the row
-__device__ __forceinline__ v4i load_k16(const int8_t *row, int k0, int K)
-{
-    if (k0 + 16 <= K) return *(const v4i_any *)(row + k0);
-    v4i r = {};
-#pragma unroll
-    for (int b = 0; b < 16; ++b)
-        if (k0 + b < K) r[b >> 2] |= (int)(uint8_t)row[k0 + b] << (8 * (b & 3));
-    return r;
-}
-
 // Wait states between the last products and their sums' first reader (see mfma_drain in conv_common.h)
 template <int N>
 __device__ __forceinline__ void drain(v4i (&acc)[N])
@@ -27,21 +16,6 @@ __device__ __forceinline__ void drain(v4i (&acc)[N])
     asm volatile("s_nop 15\n\ts_nop 3");
 #pragma unroll
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(acc[i]));
-}
-
-// One output: y[m][n] from the sums of one product, or two
-template <bool GATED>
-__device__ __forceinline__ float finish(const LinearArgs &a, int acc, int acc2, float xs, int n)
-{
-    float v = (float)acc * xs * a.ws[n];
-    if (a.bias) v += a.bias[n];
-    v = activate(v, a.act);
-    if (GATED) {
-        float v2 = (float)acc2 * xs * a.ws2[n];
-        if (a.bias2) v2 += a.bias2[n];
-        v *= v2;
-    }
-    return v;
 }
 
 // One wave a tile of 16 x 16 outputs, operands straight from memory.
@@ -77,6 +51,7 @@ __global__ __launch_bounds__(256) void linear_plain_kernel(const LinearArgs a, i
 
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st)
 {
+    if (few_linear_takes(a)) return launch_few_linear(a, st);
     if (tiled_linear_takes(a)) return launch_tiled_linear(a, st);
     const int tiles_n = (a.N + 15) / 16;
     const long long tiles = (long long)((a.M + 15) / 16) * tiles_n, blocks = (tiles + 3) / 4;
