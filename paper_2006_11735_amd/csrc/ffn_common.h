@@ -30,12 +30,17 @@ struct LinearArgs {
 
 hipError_t launch_rows(const RowsArgs &a, hipStream_t st);
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st);
+bool tokens_linear_takes(const LinearArgs &a);
+hipError_t launch_tokens_linear(const LinearArgs &a, hipStream_t st);
 bool few_linear_takes(const LinearArgs &a);
 hipError_t launch_few_linear(const LinearArgs &a, hipStream_t st);
 bool tiled_linear_takes(const LinearArgs &a);
 hipError_t launch_tiled_linear(const LinearArgs &a, hipStream_t st);
 
 typedef int v4i_any __attribute__((ext_vector_type(4), aligned(1)));       // (global memory takes 16 bytes at any address)
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef __bf16 v2b __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -44,6 +49,18 @@ __device__ __forceinline__ float load_number(const void *p, long long i, int dty
     if (dtype == kF32) return ((const float *)p)[i];
     if (dtype == kF16) return (float)((const _Float16 *)p)[i];
     return __builtin_bit_cast(float, (uint32_t)((const uint16_t *)p)[i] << 16);
+}
+
+// The same in two steps, so that no branch waits for the load: the bits, and their value
+__device__ __forceinline__ uint32_t load_bits(const void *p, long long i, int dtype)
+{
+    return dtype == kF32 ? ((const uint32_t *)p)[i] : ((const uint16_t *)p)[i];
+}
+
+__device__ __forceinline__ float value_of(uint32_t bits, int dtype)
+{
+    const float f16 = (float)__builtin_bit_cast(_Float16, (uint16_t)bits), other = __builtin_bit_cast(float, dtype == kF32 ? bits : bits << 16);
+    return dtype == kF16 ? f16 : other;
 }
 
 // (to nearest, ties to even, as the stream's 16-bit types have it; a NaN stays one)
@@ -61,15 +78,36 @@ __device__ __forceinline__ float round_number(float v, int dtype)
 
 // icnn_act.  The logistic function stands for 1 / (1 + exp(-v)): exp overflows to infinity below v = -88 and its reciprocal is the limit, 0.  The tanh
 // form of GELU is v times the logistic function of 2 sqrt(2 / pi) (v + 0.044715 v^3), since (1 + tanh t) / 2 = 1 / (1 + exp(-2 t)).
+// The erf form is v times the normal distribution's function, by formula 7.1.26 of Abramowitz and Stegun's handbook for 1 - erf(x), x = |v| / sqrt 2 (error below
+// 1.5e-7): 1 - erf(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + p x).
 __device__ __forceinline__ float logistic(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
 
-__device__ __forceinline__ float activate(float v, int act)
+template <int ACT>
+__device__ __forceinline__ float activate(float v)
 {
-    if (act == 1) return v < 0.f ? 0.f : v;
-    if (act == 2) return v * logistic(v);
-    if (act == 3) return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
-    if (act == 4) return v * logistic(1.5957691216057308f * (v + 0.044715f * v * v * v));
+    if (ACT == 1) return v < 0.f ? 0.f : v;
+    if (ACT == 2) return v * logistic(v);
+    if (ACT == 3) {
+        const float x = __builtin_fabsf(v) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
+        const float above = 0.5f * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f)))) * __expf(-x * x);
+        return v * (v < 0.f ? above : 1.f - above);
+    }
+    if (ACT == 4) return v * logistic(1.5957691216057308f * (v + 0.044715f * v * v * v));
     return v;
+}
+
+// (one branch for all: a branch a number is most of an epilogue's time)
+template <int N>
+__device__ __forceinline__ void activate_all(float (&v)[N], int act)
+{
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = f(v[e]);
+    };
+    if (act == 2) each([](float x) { return activate<2>(x); });
+    else if (act == 4) each([](float x) { return activate<4>(x); });
+    else if (act == 3) each([](float x) { return activate<3>(x); });
+    else if (act == 1) each([](float x) { return activate<1>(x); });
 }
 
 // 16 numbers k0.. of a row of K, zeros behind its end; reads no byte outside the row
@@ -83,116 +121,135 @@ __device__ __forceinline__ v4i load_k16(const int8_t *row, int k0, int K)
     return r;
 }
 
-// One output: y[m][n] from the sums of one product, or two
-template <bool GATED>
-__device__ __forceinline__ float finish(const LinearArgs &a, int acc, int acc2, float xs, int n)
+// Eight numbers of a stream of type DT: their bits, to and from float32
+template <int DT>
+struct Eight {
+    v4i b[DT == kF32 ? 2 : 1];
+};
+
+template <int DT>
+__device__ __forceinline__ Eight<DT> load_eight(const void *p, long long i)
 {
-    float v = (float)acc * xs * a.ws[n];
-    if (a.bias) v += a.bias[n];
-    v = activate(v, a.act);
-    if (GATED) {
-        float v2 = (float)acc2 * xs * a.ws2[n];
-        if (a.bias2) v2 += a.bias2[n];
-        v *= v2;
+    Eight<DT> r;
+    if constexpr (DT == kF32) {
+        r.b[0] = *(const v4i_any *)((const float *)p + i);
+        r.b[1] = *(const v4i_any *)((const float *)p + i + 4);
+    } else {
+        r.b[0] = *(const v4i_any *)((const uint16_t *)p + i);
     }
-    return v;
+    return r;
 }
 
-// Sixteen numbers from p[i] on, in the stream's type
-__device__ __forceinline__ void load_sixteen(const void *p, long long i, int dtype, float (&v)[16])
+template <int DT>
+__device__ __forceinline__ float value_of(const Eight<DT> &r, int e)
 {
-    if (dtype == kF32) {
+    if constexpr (DT == kF32) {
+        const int w = r.b[e >> 2][e & 3];          // (a bit cast of the vector's element itself takes the first one)
+        return __builtin_bit_cast(float, w);
+    } else {
+        const uint32_t w = (uint32_t)r.b[0][e >> 1];
+        if (DT == kF16) return (float)__builtin_bit_cast(_Float16, (uint16_t)(w >> (16 * (e & 1))));
+        return __builtin_bit_cast(float, e & 1 ? w & 0xffff0000u : w << 16);
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ void store_eight(void *p, long long i, const float (&v)[8])
+{
+    if constexpr (DT == kF32) {
+        *(v4f_any *)((float *)p + i) = v4f{v[0], v[1], v[2], v[3]};
+        *(v4f_any *)((float *)p + i + 4) = v4f{v[4], v[5], v[6], v[7]};
+    } else {
+        v4i t;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const v4f t = *(const v4f_any *)((const float *)p + i + 4 * q);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[4 * q + e] = t[e];
+        for (int e = 0; e < 4; ++e) {
+            const v2f two = {v[2 * e], v[2 * e + 1]};
+            t[e] = DT == kF16 ? __builtin_bit_cast(int, __builtin_convertvector(two, v2h)) : __builtin_bit_cast(int, __builtin_convertvector(two, v2b));
         }
-        return;
-    }
-    const v4i lo = *(const v4i_any *)((const uint16_t *)p + i), hi = *(const v4i_any *)((const uint16_t *)p + i + 8);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const uint16_t b = (uint16_t)((uint32_t)(e < 8 ? lo : hi)[(e & 7) >> 1] >> (16 * (e & 1)));
-        v[e] = dtype == kF16 ? (float)__builtin_bit_cast(_Float16, b) : __builtin_bit_cast(float, (uint32_t)b << 16);
+        *(v4i_any *)((uint16_t *)p + i) = t;
     }
 }
 
-__device__ __forceinline__ void store_sixteen(void *p, long long i, int dtype, const float (&v)[16])
+// The same of the `left` numbers (1 to 7) that a row still has, the last one in the others' places
+template <int DT>
+__device__ __forceinline__ Eight<DT> load_up_to_eight(const void *p, int left)
 {
-    if (dtype == kF32) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) *(v4f_any *)((float *)p + i + 4 * q) = v4f{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-        return;
-    }
-    v4i t[2];
+    Eight<DT> r = {};
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float x = v[2 * e], y = v[2 * e + 1];
-        const uint32_t b = dtype == kF16 ? __builtin_bit_cast(uint16_t, (_Float16)x) | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)y) << 16
-                                         : __builtin_bit_cast(uint16_t, (__bf16)x) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)y) << 16;
-        t[e >> 2][e & 3] = (int)b;
+        const uint32_t b = load_bits(p, min(e, left - 1), DT);
+        if (DT == kF32) r.b[DT == kF32 ? e >> 2 : 0][e & 3] = (int)b;
+        else r.b[0][e >> 1] |= (int)(b << (16 * (e & 1)));
     }
-    *(v4i_any *)((uint16_t *)p + i) = t[0];
-    *(v4i_any *)((uint16_t *)p + i + 8) = t[1];
+    return r;
 }
 
-// Sixteen scales or biases from p[n] on, the last one again behind the row's end
-__device__ __forceinline__ void load_column(const float *p, int n, int N, float (&v)[16])
+// Eight scales or biases from p[n] on
+__device__ __forceinline__ void load_column(const float *p, int n, int N, float (&v)[8])
 {
-    if (n + 16 <= N) {
-        load_sixteen(p, n, kF32, v);
-    } else {
+    const Eight<kF32> t = n + 8 <= N ? load_eight<kF32>(p, n) : load_up_to_eight<kF32>(p + n, N - n);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = p[min(n + e, N - 1)];
-    }
+    for (int e = 0; e < 8; ++e) v[e] = value_of<kF32>(t, e);
 }
 
-__device__ __forceinline__ void scale_sixteen(const int (&c)[16], float xs, const float *ws, const float *bias, int n, int N, float (&v)[16])
+// The last 16 numbers of a row, moved down so that they stand for the 16 of which `left` are left in the row, zeros behind them (left >= 16: as they are)
+__device__ __forceinline__ v4i move_down(const v4i &v, int left)
 {
-    float t[16];
-    load_column(ws, n, N, t);
+    const int over = min(max(16 - left, 0), 16);
+    v4i r;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = (float)c[e] * xs * t[e];
-    if (bias) {
-        load_column(bias, n, N, t);
+    for (int i = 0; i < 4; ++i) {
+        int lo = 0, hi = 0;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] += t[e];
-    }
-}
-
-// Outputs n .. n + 15 of row m (both inside) from their sums c, gated also c2: everything behind the sums, y written
-template <bool GATED>
-__device__ __forceinline__ void finish_sixteen(const LinearArgs &a, const int (&c)[16], const int (&c2)[16], int m, int n)
-{
-    float v[16], u[16];
-    const float xs = a.xs[m];
-    scale_sixteen(c, xs, a.ws, a.bias, n, a.N, v);
-    if (a.act != 0) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = activate(v[e], a.act);
-    }
-    if (GATED) {
-        scale_sixteen(c2, xs, a.ws2, a.bias2, n, a.N, u);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] *= u[e];
-    }
-    const long long at = m * a.ldy + n, res_at = m * a.ldr + n;
-    if (n + 16 <= a.N) {
-        if (!GATED && a.res) {
-            load_sixteen(a.res, res_at, a.dtype, u);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] += u[e];
+        for (int q = i; q < 4; ++q) {
+            lo = q == i + (over >> 2) ? v[q] : lo;
+            hi = q == i + (over >> 2) + 1 ? v[q] : hi;
         }
-        store_sixteen(a.y, at, a.dtype, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            if (n + e < a.N) {
-                if (!GATED && a.res) v[e] += load_number(a.res, res_at + e, a.dtype);
-                store_number(a.y, at + e, a.dtype, v[e]);
-            }
+        r[i] = (int)__builtin_amdgcn_alignbyte((uint32_t)hi, (uint32_t)lo, (uint32_t)(over & 3));
     }
+    return r;
+}
+
+// Outputs n .. n + 3 of row m from their sums, one product's or two: what the kernels use that have four sums of a row in a lane.  The columns' scales and
+// biases and the row's are loaded ahead (load_four), while the sums are still being taken.
+template <bool GATED>
+struct Four {
+    float xs, s1[4], b1[4], s2[4], b2[4];
+    uint32_t res[4];
+};
+
+template <bool GATED>
+__device__ __forceinline__ void load_four(const LinearArgs &a, int m, int n, Four<GATED> &f)
+{
+    f.xs = a.xs[m];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int at = min(n + e, a.N - 1);
+        f.s1[e] = a.ws[at];
+        f.b1[e] = a.bias ? a.bias[at] : 0.f;
+        if (GATED) {
+            f.s2[e] = a.ws2[at];
+            f.b2[e] = a.bias2 ? a.bias2[at] : 0.f;
+        } else {
+            f.res[e] = a.res ? load_bits(a.res, m * a.ldr + at, a.dtype) : 0;
+        }
+    }
+}
+
+template <bool GATED>
+__device__ __forceinline__ void finish_four(const LinearArgs &a, const v4i &c, const v4i &c2, const Four<GATED> &f, int m, int n)
+{
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)c[e] * f.xs * f.s1[e] + f.b1[e];
+    activate_all(v, a.act);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (n + e < a.N) {
+            if (GATED) v[e] *= (float)c2[e] * f.xs * f.s2[e] + f.b2[e];
+            else if (a.res) v[e] += value_of(f.res[e], a.dtype);
+            store_number(a.y, m * a.ldy + n + e, a.dtype, v[e]);
+        }
 }
 
 }  // namespace icnn

@@ -39,13 +39,15 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(const LinearArgs a)
     constexpr int L = GATED ? 2 : 1;                       // products
     __shared__ v4i part[NW][MT * L][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 16;
+    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
     const int8_t *w[L], *x[MT];
     w[0] = a.w + min(n0 + r, a.N - 1) * a.ldw + 16 * g;
     if (GATED) w[L - 1] = a.w2 + min(n0 + r, a.N - 1) * a.ldw + 16 * g;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) x[i] = a.x + min(16 * i + r, a.M - 1) * a.ldx + 16 * g;
+    for (int i = 0; i < MT; ++i) x[i] = a.x + min(m0 + 16 * i + r, a.M - 1) * a.ldx + 16 * g;
 
+    Four<GATED> f;                                         // of the rows 16 wave + 0..15, which this wave finishes
+    if (wave < MT) load_four<GATED>(a, min(m0 + 16 * wave + r, a.M - 1), n0 + 4 * g, f);
     v4i acc[MT * L] = {};
     auto multiply = [&](const v4i &wv, const v4i &xv, int i, int l) {
         acc[i * L + l] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, xv, acc[i * L + l], 0, 0, 0);
@@ -102,39 +104,39 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(const LinearArgs a)
     __syncthreads();
     // wave i finishes the rows 16 i + 0..15: a lane has four outputs of one
     if (wave < MT) {
-        const int m = 16 * wave + r, n = n0 + 4 * g;
+        const int m = m0 + 16 * wave + r, n = n0 + 4 * g;
         v4i c = part[0][wave * L][lane], c2 = part[0][wave * L + L - 1][lane];
 #pragma unroll
         for (int q = 1; q < NW; ++q) {
             c += part[q][wave * L][lane];
             if (GATED) c2 += part[q][wave * L + 1][lane];
         }
-        if (m < a.M) {
-            const float xs = a.xs[m];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (n + e < a.N) {
-                    float v = finish<GATED>(a, c[e], c2[e], xs, n + e);
-                    if (!GATED && a.res) v += load_number(a.res, m * a.ldr + n + e, a.dtype);
-                    store_number(a.y, m * a.ldy + n + e, a.dtype, v);
-                }
-        }
+        if (m < a.M) finish_four<GATED>(a, c, c2, f, m, n);
     }
 }
 
-bool few_linear_takes(const LinearArgs &a) { return a.M <= 64; }
+bool few_linear_takes(const LinearArgs &a) { return a.M <= 64 * 65535LL; }
 
 template <int MT, int NW, int U>
 static void launch_few(const LinearArgs &a, hipStream_t st)
 {
-    const dim3 grid((unsigned)((a.N + 15) / 16)), block(NW * 64);
+    const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 16 * MT - 1) / (16 * MT))), block(NW * 64);
     if (a.w2) hipLaunchKernelGGL((linear_few_kernel<MT, NW, U, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((linear_few_kernel<MT, NW, U, false>), grid, block, 0, st, a);
 }
 
 hipError_t launch_few_linear(const LinearArgs &a, hipStream_t st)
 {
-    if (a.M <= 16) launch_few<1, 8, 4>(a, st);
+    const int f = g_tuning.ff_few;
+    if (f == 1) launch_few<1, 16, 2>(a, st);
+    else if (f == 2) launch_few<1, 8, 2>(a, st);
+    else if (f == 3) launch_few<1, 4, 4>(a, st);
+    else if (f == 4) launch_few<1, 16, 4>(a, st);
+    else if (f == 5) launch_few<2, 8, 1>(a, st);
+    else if (f == 6) launch_few<2, 16, 1>(a, st);
+    else if (f == 7) launch_few<4, 8, 1>(a, st);
+    else if (f == 8) launch_few<4, 4, 2>(a, st);
+    else if (a.M <= 16) launch_few<1, 8, 4>(a, st);
     else if (a.M <= 32) launch_few<2, 8, 2>(a, st);
     else launch_few<4, 8, 2>(a, st);
     return hipGetLastError();

@@ -38,21 +38,17 @@ __global__ __launch_bounds__(256) void linear_plain_kernel(const LinearArgs a, i
     drain(acc);
     const int m = m0 + r;
     if (m >= a.M) return;
-    const float xs = a.xs[m];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int n = n0 + 4 * g + i;
-        if (n >= a.N) break;
-        float v = finish<GATED>(a, acc[0][i], acc[1][i], xs, n);
-        if (!GATED && a.res) v += load_number(a.res, m * a.ldr + n, a.dtype);
-        store_number(a.y, m * a.ldy + n, a.dtype, v);
-    }
+    Four<GATED> f;
+    load_four<GATED>(a, m, n0 + 4 * g, f);
+    finish_four<GATED>(a, acc[0], acc[1], f, m, n0 + 4 * g);
 }
 
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st)
 {
-    if (few_linear_takes(a)) return launch_few_linear(a, st);
-    if (tiled_linear_takes(a)) return launch_tiled_linear(a, st);
+    const int force = g_tuning.ff_kernel;
+    if (tokens_linear_takes(a) && (force == 7 || force == 0)) return launch_tokens_linear(a, st);
+    if (few_linear_takes(a) && (force == 2 || (force == 0 && a.M <= 64))) return launch_few_linear(a, st);
+    if (tiled_linear_takes(a) && force != 1) return launch_tiled_linear(a, st);
     const int tiles_n = (a.N + 15) / 16;
     const long long tiles = (long long)((a.M + 15) / 16) * tiles_n, blocks = (tiles + 3) / 4;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const RowsArgs a)
 
 // Eight numbers of the stream from p[i] on, to and from float32
 template <int DT>
-__device__ __forceinline__ void load_eight(const void *p, long long i, float (&v)[8])
+__device__ __forceinline__ void stream_eight(const void *p, long long i, float (&v)[8])
 {
     if (DT == kF32) {
 #pragma unroll
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256) void rows_held_kernel(const RowsArgs a)
     for (int k = 0; k < V; ++k) {
         const int i = 8 * (k * T + t);
         if (i + 8 <= a.c) {
-            load_eight<DT>(a.x, row * a.ldx + i, v[k]);
+            stream_eight<DT>(a.x, row * a.ldx + i, v[k]);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[k][e] = i + e < a.c ? load_number(a.x, row * a.ldx + i + e, DT) : 0.f;
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(256) void rows_held_kernel(const RowsArgs a)
         for (int k = 0; k < V; ++k) {
             const int i = 8 * (k * T + t);
             if (i + 8 <= a.c) {
-                load_eight<DT>(a.res, row * a.ldr + i, u[k]);
+                stream_eight<DT>(a.res, row * a.ldr + i, u[k]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) u[k][e] = i + e < a.c ? load_number(a.res, row * a.ldr + i + e, DT) : 0.f;
@@ -181,8 +181,8 @@ __global__ __launch_bounds__(256) void rows_held_kernel(const RowsArgs a)
             const int i = 8 * (k * T + t);
             float gm[8];
             if (i + 8 <= a.c) {
-                if (DT == kF32 || a.gamma_dtype == DT) load_eight<DT>(a.gamma, i, gm);
-                else load_eight<kF32>(a.gamma, i, gm);
+                if (DT == kF32 || a.gamma_dtype == DT) stream_eight<DT>(a.gamma, i, gm);
+                else stream_eight<kF32>(a.gamma, i, gm);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) gm[e] = i + e < a.c ? load_number(a.gamma, i + e, a.gamma_dtype) : 0.f;

@@ -6,6 +6,8 @@
 // In a gated layer the 32-row groups of a tile's weights are gate and up in turn, so a wave holds both sums of an output in the same lane and register.
 #include "ffn_common.h"
 
+#include <type_traits>
+
 namespace icnn {
 
 namespace {
@@ -20,13 +22,25 @@ struct TiledArgs {
     int tiles_n, tiles_m, per_xcd;
 };
 
-// Where row q's 16-byte piece c lies in its stage.  Eight lanes that read the same piece of eight rows, as the fragments of either operand have them (rows
-// 8 i + 0..7, or of the weights 0..3 and 16..19), find them in eight different pieces of the 128 bytes that LDS hands out together.
+// Row q's 16-byte piece c lies at c ^ piece_key(q) in its stage.  LDS hands out 256 bytes at a time, the pieces of sixteen lanes: those read the same piece of sixteen
+// rows, as the fragments of either operand have them (rows 16 i + 0..15, of the weights 0..3, 16..19, 4..7, 20..23), and find them in sixteen different places
+// of the 256 bytes.
 template <int BK, bool WEIGHTS>
 __device__ __forceinline__ int piece_key(int q)
 {
-    if (BK == 128) return WEIGHTS ? (q & 3) | ((q >> 4) & 1) << 2 : q & 7;
-    return WEIGHTS ? ((q >> 1) & 1) | ((q >> 4) & 1) << 1 : (q >> 1) & 3;
+    if (BK == 128) return WEIGHTS ? ((q >> 1) & 3) | ((q >> 4) & 1) << 2 : (q >> 1) & 7;
+    return WEIGHTS ? ((q >> 2) & 1) | ((q >> 4) & 1) << 1 : (q >> 2) & 3;
+}
+
+// The 16 numbers from p on of a row of which `left` are left (any number, also none or less), zeros behind them.  The row has 16 numbers at least: its last 16
+// are read and moved down.
+__device__ __forceinline__ v4i last_k16(const int8_t *p, int left) { return move_down(*(const v4i_any *)(p - max(16 - left, 0)), left); }
+
+// Waves a SIMD when as many workgroups of `waves` waves as their LDS lets share a compute unit do (three at most: the registers are wanted too)
+constexpr int waves_per_simd(int waves, int lds_bytes)
+{
+    const int groups = 163840 / lds_bytes < 3 ? 163840 / lds_bytes : 3;
+    return groups * waves < 4 ? 1 : groups * waves / 4;
 }
 
 template <int TN, int TM>
@@ -45,11 +59,13 @@ __device__ __forceinline__ void drain(v16i (&acc)[TN][TM])
 
 }  // namespace
 
-template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED>
-__global__ __launch_bounds__(WN * WM * 64, 1) void linear_tiled_kernel(const TiledArgs ta)
+template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED, bool DIRECT>
+__global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN + TM * WM) * BK * STAGES)) void linear_tiled_kernel(const TiledArgs ta)
 {
+#if defined(__HIP_DEVICE_COMPILE__)   // the buffer-resource type exists in the device pass only
     constexpr int NW = WN * WM, BN = 32 * TN * WN, BM = 32 * TM * WM, ROWS = 1024 / BK, PIECES = BK / 16, SLICES = BK / 32;
-    constexpr int LW = BN / ROWS / NW, LX = BM / ROWS / NW, LOADS = LW + LX, STAGE = (BN + BM) * BK, LDS_GROUPS = STAGES * STAGE / 4096;
+    constexpr int LW = BN / ROWS / NW, LX = BM / ROWS / NW, LOADS = LW + LX, STAGE = (BN + BM) * BK;
+    static_assert(DIRECT || STAGES == 2, "copies through registers are one stage ahead");
     static_assert(LW * ROWS * NW == BN && LX * ROWS * NW == BM && SLICES >= 2 && SLICES % 2 == 0, "whole copies, two fragment sets in turn");
     extern __shared__ __align__(1024) uint8_t lds[];
     const LinearArgs &a = ta.l;
@@ -85,21 +101,49 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void linear_tiled_kernel(const Til
         off_x[j] = (unsigned)min(q, a.M - 1 - m0) * (unsigned)a.ldx + 16 * piece_x[j];
     }
     const int steps = (a.K + BK - 1) / BK;
-    auto copy_step = [&](int s) {
-        uint8_t *const to = lds + (s % STAGES) * STAGE + wave * 1024;
+    // copies FROM .. TO - 1 of step s: of the weights, then of the rows.  Behind the last step nothing but zeros comes.
+    auto copy_part = [&](int s, auto from, auto to) {
+        uint8_t *const at = lds + (s % STAGES) * STAGE + wave * 1024;
+        const int k0 = s * BK, left = a.K - k0;
+#pragma unroll
+        for (int j = from; j < to; ++j) {
+            if (j < LW) {
+                const bool up = GATED && (((j * NW + wave) * ROWS) & 32);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(up ? rs_w2 : rs_w, (LdsVoid *)(at + j * NW * 1024), 16, 16 * piece_w[j] < left ? off_w[j] : 0x80000000u, k0, 0, 0);
+            } else {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_x, (LdsVoid *)(at + BN * BK + (j - LW) * NW * 1024), 16, 16 * piece_x[j - LW] < left ? off_x[j - LW] : 0x80000000u,
+                                                         k0, 0, 0);
+            }
+        }
+    };
+    // The same through registers, for rows that start anywhere: fetch_step's loads are in flight while a stage is multiplied, put_step's stores follow
+    v4i held[LOADS];
+    auto fetch_step = [&](int s) {
         const int k0 = s * BK;
-        const bool whole = k0 + BK <= a.K;
+        const int8_t *const w0 = a.w + n0 * a.ldw + k0, *const w1 = (GATED ? a.w2 : a.w) + n0 * a.ldw + k0, *const x0 = a.x + m0 * a.ldx + k0;
+        if (k0 + BK <= a.K) {
 #pragma unroll
-        for (int j = 0; j < LW; ++j) {
-            const unsigned off = whole || k0 + 16 * piece_w[j] < a.K ? off_w[j] : 0x80000000u;
-            const bool up = GATED && (((j * NW + wave) * ROWS) & 32);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(up ? rs_w2 : rs_w, (LdsVoid *)(to + j * NW * 1024), 16, off, k0, 0, 0);
-        }
+            for (int j = 0; j < LW; ++j) {
+                const bool up = GATED && (((j * NW + wave) * ROWS) & 32);
+                held[j] = *(const v4i_any *)((up ? w1 : w0) + off_w[j]);
+            }
 #pragma unroll
-        for (int j = 0; j < LX; ++j) {
-            const unsigned off = whole || k0 + 16 * piece_x[j] < a.K ? off_x[j] : 0x80000000u;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_x, (LdsVoid *)(to + BN * BK + j * NW * 1024), 16, off, k0, 0, 0);
+            for (int j = 0; j < LX; ++j) held[LW + j] = *(const v4i_any *)(x0 + off_x[j]);
+        } else {
+            const int left = a.K - k0;
+#pragma unroll
+            for (int j = 0; j < LW; ++j) {
+                const bool up = GATED && (((j * NW + wave) * ROWS) & 32);
+                held[j] = last_k16((up ? w1 : w0) + off_w[j], left - 16 * piece_w[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < LX; ++j) held[LW + j] = last_k16(x0 + off_x[j], left - 16 * piece_x[j]);
         }
+    };
+    auto put_step = [&](int s) {
+        uint8_t *const to = lds + (s % STAGES) * STAGE + wave * 1024 + lane * 16;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) *(v4i *)(to + (j < LW ? j * NW * 1024 : BN * BK + (j - LW) * NW * 1024)) = held[j];
     };
 
     // ---- fragments: lane l has row l % 32 of its group and the 16 bytes l / 32 of a slice of 32.  Weight row r of a group is n = 16 ((r >> 2) & 1) +
@@ -123,75 +167,214 @@ __global__ __launch_bounds__(WN * WM * 64, 1) void linear_tiled_kernel(const Til
             for (int j = 0; j < TM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[set][i], fx[set][j], acc[i][j], 0, 0, 0);
     };
 
+    // The order of a slice's products, the reads of the next one's fragments and the copies among them: reads under the first half of the products, copies under
+    // the second, so that neither queue stops the wave between two products.
+    auto order = [&](auto copies) {
+        constexpr int M = TN * TM, R = TN + TM, H = M / 2, C = copies;
 #pragma unroll
-    for (int s = 0; s < STAGES; ++s)
-        if (s < steps) copy_step(s);
-    if (steps >= STAGES) FFN_WAIT_VMCNT((STAGES - 1) * LOADS);
-    else FFN_WAIT_VMCNT(0);
+        for (int m = 0; m < M; ++m) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            const int reads = m < H ? R * (m + 1) / H - R * m / H : 0, cs = m < H ? 0 : C * (m - H + 1) / (M - H) - C * (m - H) / (M - H);
+            if (reads == 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (reads == 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            if (reads >= 3) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+            if (cs == 1) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+            if (cs == 2) __builtin_amdgcn_sched_group_barrier(0x010, 2, 0);
+            if (cs >= 3) __builtin_amdgcn_sched_group_barrier(0x010, 4, 0);
+        }
+    };
+    typedef std::integral_constant<int, 0> None;
+    typedef std::integral_constant<int, LOADS / 2> Half;
+    typedef std::integral_constant<int, LOADS> All;
+    if (DIRECT) {
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s)
+            if (s < STAGES - 1) copy_part(s, None{}, All{});
+            else copy_part(s, None{}, Half{});
+        FFN_WAIT_VMCNT((STAGES - 2) * LOADS + LOADS / 2);
+    } else {
+        fetch_step(0);
+        put_step(0);
+        if (1 < steps) fetch_step(1);
+        FFN_WAIT_LGKM();
+    }
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     read_slice(0, 0, 0);
-    // A stage's last slice is multiplied behind the barrier: its fragments have left LDS in front of it, so the stage is free for the copies issued there,
-    // and the first fragments of the next one come in under those products.
+    // A stage's last slice is multiplied behind the barrier: its fragments have left LDS in front of it, so the stage is free for the copies of the step STAGES
+    // further on (half of them there, half in the next step's first slice), and the first fragments of the next step come in under those products.
     for (int s = 0; s < steps; ++s) {
 #pragma unroll
         for (int kk = 0; kk < SLICES - 1; ++kk) {
             read_slice(s % STAGES, kk + 1, (kk + 1) & 1);
+            if (DIRECT && kk == 0) copy_part(s + STAGES - 1, Half{}, All{});
             multiply(kk & 1);
+            if (DIRECT && kk == 0) order(std::integral_constant<int, LOADS - LOADS / 2>{});
+            else order(None{});
         }
-        if (s + 1 < steps) {
-            if (s + STAGES <= steps) FFN_WAIT_VMCNT((STAGES - 2) * LOADS);      // (the stages behind the next one are still in flight)
-            else FFN_WAIT_VMCNT(0);
-            FFN_WAIT_LGKM();
-            __builtin_amdgcn_s_barrier();
-            if (s + STAGES < steps) copy_step(s + STAGES);
-            read_slice((s + 1) % STAGES, 0, 0);
-        }
+        if (DIRECT) FFN_WAIT_VMCNT((STAGES - 2) * LOADS);              // (the stages behind the next one are still in flight)
+        else if (s + 1 < steps) put_step(s + 1);
+        FFN_WAIT_LGKM();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        read_slice((s + 1) % STAGES, 0, 0);
+        if (DIRECT) copy_part(s + STAGES, None{}, Half{});
+        else if (s + 2 < steps) fetch_step(s + 2);
         multiply(1);
+        if (DIRECT) order(Half{});
     }
+    FFN_WAIT_VMCNT(0);
     drain(acc);
 
-    // ---- epilogue.  The sums go through LDS, every lane's own back to itself, only so that a loop can run over them: one body of code for all groups.
-    constexpr int GROUPS = TN * TM, ROUND = LDS_GROUPS / NW < GROUPS ? LDS_GROUPS / NW : GROUPS;
-    static_assert(GROUPS % ROUND == 0 && ROUND % TN == 0, "whole columns of groups a round");
-    __syncthreads();
-    uint8_t *const mine = lds + wave * ROUND * 4096 + lane * 16;
-#pragma unroll
-    for (int j0 = 0; j0 < TM; j0 += ROUND / TN) {
-#pragma unroll
-        for (int g = 0; g < ROUND; ++g)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const v16i &c = acc[g % TN][j0 + g / TN];
-                *(v4i *)(mine + g * 4096 + q * 1024) = v4i{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
-            }
-#pragma unroll 1
-        for (int g = 0; g < ROUND; g += GATED ? 2 : 1) {
-            const int i = g % TN, m = m0 + (wm * TM + j0 + g / TN) * 32 + r;
-            const int n = n0 + (wn * TN + i) * (GATED ? 16 : 32) + 16 * half;
-            int c[16], c2[16];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const v4i t = *(const v4i *)(mine + g * 4096 + q * 1024), u = GATED ? *(const v4i *)(mine + (g + 1) * 4096 + q * 1024) : v4i{};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    c[4 * q + e] = t[e];
-                    c2[4 * q + e] = u[e];
-                }
-            }
-            if (m < a.M && n < a.N) finish_sixteen<GATED>(a, c, c2, m, n);
+    // ---- epilogue.  The sums go through LDS (as many of the tile's rows at a time as fit) into an order in which a thread has eight outputs n next to each
+    // other of row after row: it reads their scales and biases once, a row's residual and y are read and written in whole lines, and the loads of several rows are in
+    // flight together.  Row q's 16-byte piece c lies at c ^ (q & 15).
+    constexpr int OUT = GATED ? BN / 2 : BN, TPR = OUT / 8, PASS = NW * 64 / TPR;           // outputs, threads a row; rows a pass
+    constexpr int FIT = STAGES * STAGE / (WM * 32 * BN * 4), JR = FIT >= TM ? TM : FIT >= 2 && TM % 2 == 0 ? 2 : 1, ROWS_R = WM * JR * 32;
+    static_assert(FIT >= 1 && ROWS_R % (PASS * 2) == 0 && TM <= 4, "whole passes, at most four dumps");
+    const int o = 8 * (threadIdx.x % TPR), q0 = threadIdx.x / TPR, n = n0 + o;
+    const int c0 = (GATED ? (o >> 5) * 64 + (o & 31) : o) >> 2;                             // first piece of the thread's sums
+    const bool some = n < a.N, all = n + 8 <= a.N;
+    float s1[8] = {}, b1[8] = {}, s2[8] = {}, b2[8] = {};
+    if (some) {
+        load_column(a.ws, n, a.N, s1);
+        if (a.bias) load_column(a.bias, n, a.N, b1);
+        if (GATED) {
+            load_column(a.ws2, n, a.N, s2);
+            if (a.bias2) load_column(a.bias2, n, a.N, b2);
         }
     }
+    auto barrier = [&]() {
+        FFN_WAIT_LGKM();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // P rows of a thread at a time; the residual of the next ones is on its way
+    const bool with_res = !GATED && a.res;
+    auto dump = [&](auto j0) {
+#pragma unroll
+        for (int j = 0; j < JR; ++j)
+#pragma unroll
+            for (int i = 0; i < TN; ++i) {
+                const int q = (wm * JR + j) * 32 + r, c = (wn * TN + i) * 8 + 4 * half;
+                const v16i &t = acc[i][j0 + j];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *(v4i *)(lds + q * (BN * 4) + (((c + e) ^ (q & 15)) << 4)) = v4i{t[4 * e], t[4 * e + 1], t[4 * e + 2], t[4 * e + 3]};
+            }
+    };
+    auto finish = [&](auto dt) {
+        constexpr int DT = dt, P = 2, TURNS = ROWS_R / PASS / P, ALL_TURNS = TM / JR * TURNS, DEPTH = ALL_TURNS % 2 ? 1 : 2, ITEM = DT == kF32 ? 4 : 2;
+        // row q0 + (a number that is the same for all threads) of the tile
+        static_assert(32 % PASS == 0 && P * PASS % 16 == 0, "a pass stays in a group's 32 rows, a turn's rows start at a multiple of 16");
+        auto above = [&](int turn, int p) {
+            const int q = ((turn % TURNS) * P + p) * PASS;
+            return (q / (JR * 32) * TM + turn / TURNS * JR) * 32 + q % (JR * 32);
+        };
+        const int last = some ? a.M - m0 - q0 : 0;                                          // rows from the thread's first one on
+        const float *const xs0 = a.xs + m0 + q0;
+        const uint8_t *const res0 = (const uint8_t *)a.res + ((m0 + q0) * a.ldr + n) * ITEM;
+        uint8_t *const y0 = (uint8_t *)a.y + ((m0 + q0) * a.ldy + n) * ITEM;
+        Eight<DT> ahead[DEPTH][P] = {};
+        float xs_ahead[DEPTH][P] = {};
+        auto fetch = [&](int turn, int to) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int u = above(turn, p);
+                if (u < last) {
+                    xs_ahead[to][p] = xs0[u];
+                    if (with_res) ahead[to][p] = all ? load_eight<DT>(res0 + u * a.ldr * ITEM, 0) : load_up_to_eight<DT>(res0 + u * a.ldr * ITEM, a.N - n);
+                }
+            }
+        };
+        auto one_turn = [&](int turn, auto slot) {
+            if (turn && turn % TURNS == 0) {
+                barrier();
+                if (JR < TM && turn == TURNS) dump(std::integral_constant<int, (JR < TM ? JR : 0)>{});
+                if (2 * JR < TM && turn == 2 * TURNS) dump(std::integral_constant<int, (2 * JR < TM ? 2 * JR : 0)>{});
+                if (3 * JR < TM && turn == 3 * TURNS) dump(std::integral_constant<int, (3 * JR < TM ? 3 * JR : 0)>{});
+                barrier();
+            }
+            const uint8_t *const from = lds + ((turn % TURNS) * P * PASS + q0) * (BN * 4);
+            Eight<DT> res[P];
+            float v[P * 8], xs[P];
+            v4i t[P][GATED ? 4 : 2];
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                res[p] = ahead[slot][p];
+                xs[p] = xs_ahead[slot][p];
+#pragma unroll
+                for (int e = 0; e < (GATED ? 4 : 2); ++e)
+                    t[p][e] = *(const v4i *)(from + p * PASS * (BN * 4) + (((c0 + (e & 1) + (e & 2) * 4) ^ ((q0 + p * PASS) & 15)) << 4));
+            }
+            if (turn + DEPTH < ALL_TURNS) fetch(turn + DEPTH, slot);
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[8 * p + e] = (float)t[p][e >> 2][e & 3] * xs[p] * s1[e] + b1[e];
+            activate_all(v, a.act);
+            if (GATED) {
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[8 * p + e] *= (float)t[p][GATED ? 2 + (e >> 2) : 0][e & 3] * xs[p] * s2[e] + b2[e];
+            }
+            if (with_res) {
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[8 * p + e] += value_of<DT>(res[p], e);
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int u = above(turn, p);
+                float out[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) out[e] = v[8 * p + e];
+                if (u < last) {
+                    uint8_t *const at = y0 + u * a.ldy * ITEM;
+                    if (all) {
+                        store_eight<DT>(at, 0, out);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 7; ++e)
+                            if (n + e < a.N) store_number(at, e, DT, out[e]);
+                    }
+                }
+            }
+        };
+#pragma unroll
+        for (int k = 0; k < DEPTH; ++k) fetch(k, k);
+        barrier();
+        dump(std::integral_constant<int, 0>{});
+        barrier();
+#pragma unroll 1
+        for (int turn = 0; turn < ALL_TURNS; turn += DEPTH) {
+            one_turn(turn, std::integral_constant<int, 0>{});
+            if constexpr (DEPTH == 2) one_turn(turn + 1, std::integral_constant<int, DEPTH - 1>{});
+        }
+    };
+    if (a.dtype == kBf16) finish(std::integral_constant<int, kBf16>{});
+    else if (a.dtype == kF16) finish(std::integral_constant<int, kF16>{});
+    else finish(std::integral_constant<int, kF32>{});
+#endif
 }
 
-// Rows and weights that start at multiples of 16 bytes, with whole 16-byte pieces of k; a tile's rows within 2 GiB
-bool tiled_linear_takes(const LinearArgs &a)
+// Offsets in a tile's rows within 2 GiB; k is at least a piece
+bool tiled_linear_takes(const LinearArgs &a) { return a.K >= 16 && a.ldx <= (1 << 22) && a.ldw <= (1 << 22); }
+
+// Rows and weights that start at multiples of 16 bytes, with whole 16-byte pieces of k, are copied without a stop in registers
+static bool direct(const LinearArgs &a)
 {
     const uintptr_t at = (uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.w2;
-    return a.M > 64 && (at & 15) == 0 && ((a.ldx | a.ldw | a.K) & 15) == 0 && a.ldx <= (1 << 22) && a.ldw <= (1 << 22);
+    return (at & 15) == 0 && ((a.ldx | a.ldw | a.K) & 15) == 0;
 }
 
-template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED>
-static hipError_t launch_tiles(const LinearArgs &a, hipStream_t st)
+template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED, bool DIRECT>
+static hipError_t launch_one(const LinearArgs &a, hipStream_t st)
 {
     constexpr int BN = 32 * TN * WN / (GATED ? 2 : 1), BM = 32 * TM * WM, LDS = 32 * (TN * WN + TM * WM) * BK * STAGES;
     TiledArgs t;
@@ -201,14 +384,58 @@ static hipError_t launch_tiles(const LinearArgs &a, hipStream_t st)
     const long long tiles = (long long)t.tiles_n * t.tiles_m, per = (tiles + 7) / 8;
     if (tiles > 0x7ffffff0LL) return hipErrorInvalidValue;
     t.per_xcd = (int)per;
-    auto *const k = linear_tiled_kernel<TN, TM, WN, WM, BK, STAGES, GATED>;
+    auto *const k = linear_tiled_kernel<TN, TM, WN, WM, BK, STAGES, GATED, DIRECT>;
+    if (LDS > 65536)
+        if (hipError_t e = allow_large_lds((const void *)k)) return e;
     hipLaunchKernelGGL(k, dim3((unsigned)(per * 8)), dim3(WN * WM * 64), LDS, st, t);
     return hipGetLastError();
 }
 
+template <int TN, int TM, int WN, int WM, int BK, int STAGES>
+static hipError_t launch_tiles(const LinearArgs &a, hipStream_t st)
+{
+    if (direct(a)) return a.w2 ? launch_one<TN, TM, WN, WM, BK, STAGES, true, true>(a, st) : launch_one<TN, TM, WN, WM, BK, STAGES, false, true>(a, st);
+    return a.w2 ? launch_one<TN, TM, WN, WM, 128, 2, true, false>(a, st) : launch_one<TN, TM, WN, WM, 128, 2, false, false>(a, st);
+}
+
+// Which tile.  A tile's time is a part that does not depend on k (start, epilogue) and one for each 128 bytes of k; tiles beyond what the 256 compute units
+// hold at a time wait for another turn.  Measured in us: {rows, weight rows, held at a time, fixed, a step with few tiles on the chip, a step with all}.
+struct TileCost {
+    int m, n, held;
+    float fixed, few, all;
+};
+constexpr TileCost kTiles[] = {
+    {256, 256, 256, 12.f, 1.15f, 1.7f},     // 4096 x 4096 -> 4096: 73 us (the next one: 87); 512 x 4096 -> 4096: 66
+    {128, 128, 512, 6.f, 0.65f, 0.96f},     // gated 512 x 4096 -> 8192: 46 us (the one before 59, the next one 56)
+    {64, 128, 512, 4.f, 0.45f, 0.65f},      // 512 x 4096 -> 4096: 20.6 us (the one before 28.5), 1024 x 4096 -> 4096: 31 us (39 and, by the next one, 41)
+    {64, 64, 512, 3.5f, 0.45f, 0.5f},       // 128 x 4096 -> 4096: 16.8 us (the one before 18.2)
+};
+
+static int choose_tile(const LinearArgs &a)
+{
+    int best = 0;
+    float least = 0.f;
+    for (int c = 0; c < 4; ++c) {
+        const TileCost &t = kTiles[c];
+        const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + t.n - 1) / t.n), turns = __builtin_ceilf(tiles / (float)t.held);
+        const float full = tiles < (float)t.held ? tiles / (float)t.held : 1.f;
+        const float us = turns * (t.fixed + (float)((a.K + 127) / 128) * (t.few + (t.all - t.few) * full));
+        if (c == 0 || us < least) {
+            least = us;
+            best = c;
+        }
+    }
+    return best;
+}
+
 hipError_t launch_tiled_linear(const LinearArgs &a, hipStream_t st)
 {
-    return a.w2 ? launch_tiles<4, 4, 2, 2, 128, 2, true>(a, st) : launch_tiles<4, 4, 2, 2, 128, 2, false>(a, st);
+    switch (g_tuning.ff_kernel >= 3 ? g_tuning.ff_kernel - 3 : choose_tile(a)) {
+    case 0: return launch_tiles<2, 4, 4, 2, 128, 2>(a, st);
+    case 1: return launch_tiles<2, 2, 2, 2, 128, 2>(a, st);
+    case 2: return launch_tiles<2, 1, 2, 2, 128, 3>(a, st);
+    default: return launch_tiles<2, 1, 1, 2, 128, 4>(a, st);
+    }
 }
 
 }  // namespace icnn

@@ -1,0 +1,145 @@
+// Products of up to four 8-bit rows and weights (see ffn_linear.hip for the mathematics): the single tokens of a decoder.  Nothing but the weights' way from memory
+// counts.  A wave reads whole kilobytes of a weight row an instruction (16 bytes a lane), all of its rows' in flight at once, against the rows' pieces that it
+// keeps in registers; sums are taken four products an instruction (v_dot4) and joined over the lanes at the end, over the KW waves that share the k axis in LDS.
+#include "ffn_common.h"
+
+namespace icnn {
+
+namespace {
+
+// The sum over a wave's lanes, in every lane: over rows of sixteen by moves within the row, over the four rows by scalar reads
+__device__ __forceinline__ int sum_of_lanes(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true);       // lanes ^ 1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true);       // lanes ^ 2
+    v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true);      // the other half of eight, mirrored
+    v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true);      // the other half of sixteen, mirrored
+    return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) + (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
+}
+
+}  // namespace
+
+// MR rows; C kilobytes of k a wave, KW waves along k; OUT outputs a wave
+template <int MR, int C, int KW, int OUT, bool GATED>
+__global__ __launch_bounds__(256) void linear_tokens_kernel(const LinearArgs a)
+{
+    constexpr int L = GATED ? 2 : 1;
+    __shared__ int part[4][OUT * L * MR];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = ((int)blockIdx.x * (4 / KW) + wave / KW) * OUT;      // (may lie behind the last output: nothing is stored then)
+    // the pieces' places in a row; a piece that goes beyond its end is read as the row's last 16 bytes and moved down, zeros behind
+    int at[C], left[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int k = ((wave % KW) * C + c) * 1024 + 16 * lane;
+        left[c] = a.K - k;
+        at[c] = min(k, a.K - 16);
+    }
+    const bool whole = (a.K & 15) == 0;
+    v4i x[MR][C], w[OUT][L][C];
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            x[m][c] = *(const v4i_any *)(a.x + min(m, a.M - 1) * a.ldx + at[c]);
+        }
+#pragma unroll
+    for (int b = 0; b < OUT; ++b)
+#pragma unroll
+        for (int l = 0; l < L; ++l)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                w[b][l][c] = __builtin_nontemporal_load((const v4i_any *)((l ? a.w2 : a.w) + min(n0 + b, a.N - 1) * a.ldw + at[c]));
+    // what the lane that will finish output j % OUT of row j / OUT needs
+    const int fm = min(lane / OUT, a.M - 1), fn = min(n0 + lane % OUT, a.N - 1);
+    const bool finishes = lane < OUT * MR && wave % KW == 0 && lane / OUT < a.M && n0 + lane % OUT < a.N;
+    float xs = 0.f, s1 = 0.f, b1 = 0.f, s2 = 0.f, b2 = 0.f;
+    uint32_t res = 0;
+    if (finishes) {
+        xs = a.xs[fm];
+        s1 = a.ws[fn];
+        if (a.bias) b1 = a.bias[fn];
+        if (GATED) {
+            s2 = a.ws2[fn];
+            if (a.bias2) b2 = a.bias2[fn];
+        } else if (a.res) {
+            res = load_bits(a.res, fm * a.ldr + fn, a.dtype);
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+        for (int c = 0; c < C; ++c) x[m][c] = whole ? (left[c] > 0 ? x[m][c] : v4i{}) : move_down(x[m][c], left[c]);
+    if (!whole) {
+#pragma unroll
+        for (int b = 0; b < OUT; ++b)
+#pragma unroll
+            for (int l = 0; l < L; ++l)
+#pragma unroll
+                for (int c = 0; c < C; ++c) w[b][l][c] = move_down(w[b][l][c], left[c]);
+    }
+#pragma unroll
+    for (int b = 0; b < OUT; ++b)
+#pragma unroll
+        for (int l = 0; l < L; ++l)
+#pragma unroll
+            for (int m = 0; m < MR; ++m) {
+                int s = 0;
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_sdot4(w[b][l][c][e], x[m][c][e], s, false);
+                s = sum_of_lanes(s);
+                if (lane == 0) part[wave][(m * OUT + b) * L + l] = s;
+            }
+    __syncthreads();
+    if (finishes) {
+        int c1 = 0, c2 = 0;
+#pragma unroll
+        for (int q = 0; q < KW; ++q) {
+            c1 += part[wave + q][lane * L];
+            if (GATED) c2 += part[wave + q][lane * L + 1];
+        }
+        float v[1] = {(float)c1 * xs * s1 + b1};
+        activate_all(v, a.act);
+        if (GATED) v[0] *= (float)c2 * xs * s2 + b2;
+        else if (a.res) v[0] += value_of(res, a.dtype);
+        store_number(a.y, fm * a.ldy + fn, a.dtype, v[0]);
+    }
+}
+
+bool tokens_linear_takes(const LinearArgs &a) { return a.M <= 4 && a.K >= 16 && a.K <= 32768; }
+
+template <int MR, int C, int KW, int OUT>
+static void launch_tokens(const LinearArgs &a, hipStream_t st)
+{
+    const dim3 grid((unsigned)((a.N + OUT * (4 / KW) - 1) / (OUT * (4 / KW)))), block(256);
+    if (a.w2) {
+        constexpr int HALF = OUT / 2 < 1 ? 1 : OUT / 2;
+        const dim3 wide((unsigned)((a.N + HALF * (4 / KW) - 1) / (HALF * (4 / KW))));
+        hipLaunchKernelGGL((linear_tokens_kernel<MR, C, KW, HALF, true>), wide, block, 0, st, a);
+    } else {
+        hipLaunchKernelGGL((linear_tokens_kernel<MR, C, KW, OUT, false>), grid, block, 0, st, a);
+    }
+}
+
+template <int MR>
+static void launch_rows_of(const LinearArgs &a, hipStream_t st)
+{
+    if (a.K <= 1024) launch_tokens<MR, 1, 1, 8>(a, st);
+    else if (a.K <= 2048) launch_tokens<MR, 2, 1, 8>(a, st);
+    else if (a.K <= 4096) launch_tokens<MR, 4, 1, 4>(a, st);
+    else if (a.K <= 8192) launch_tokens<MR, 4, 2, 4>(a, st);
+    else if (a.K <= 16384) launch_tokens<MR, 4, 4, 4>(a, st);
+    else launch_tokens<MR, 8, 4, 2>(a, st);
+}
+
+hipError_t launch_tokens_linear(const LinearArgs &a, hipStream_t st)
+{
+    if (a.M == 1) launch_rows_of<1>(a, st);
+    else if (a.M == 2) launch_rows_of<2>(a, st);
+    else launch_rows_of<4>(a, st);
+    return hipGetLastError();
+}
+
+}  // namespace icnn
