@@ -149,6 +149,8 @@ const char *icnn_last_error(void);
  *   "keep"        0 library's choice; 1 / 2: every / no layer whose shape it takes on the 3x3 kernel that keeps 64 channels' weights in registers
  *   "flat"        0 library's choice; 1 / 2: every / no layer whose shape it takes on the kernel that streams weights into registers
  *   "tri_tile"    0 library's choice; 1..4 = the 3x3 + 1x1 + 1x1 kernel at any size, in tiles of 32, 64, 96 or 112 pixels
+ *   "ff_kernel"   0 library's choice; products of 8-bit rows, where the shape allows it, by 1 the plain kernel, 2 the one for up to four rows, 3 the one for up to 64
+ *                 rows, 4, 5, 6, 7 in tiles of 256 x 256, 128 x 128, 64 x 128, 64 x 64 rows x weight rows
  *   "ksplit"      0, 1 never split the K axis over workgroups (the library's choice); 2..8 that split where it divides the K steps
  *   "reset"       (value ignored) back to the library's choices
  * Unknown names and values outside these ranges return ICNN_E_PARAM and change nothing. */

@@ -30,11 +30,14 @@ struct LinearArgs {
 
 hipError_t launch_rows(const RowsArgs &a, hipStream_t st);
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st);
+// kernels of ffn_tokens.hip, ffn_few.hip and ffn_tiled.hip: whether they take a product's shape, and about how long it takes them
 bool tokens_linear_takes(const LinearArgs &a);
 hipError_t launch_tokens_linear(const LinearArgs &a, hipStream_t st);
 bool few_linear_takes(const LinearArgs &a);
+float few_linear_us(const LinearArgs &a);
 hipError_t launch_few_linear(const LinearArgs &a, hipStream_t st);
 bool tiled_linear_takes(const LinearArgs &a);
+float tiled_linear_us(const LinearArgs &a);
 hipError_t launch_tiled_linear(const LinearArgs &a, hipStream_t st);
 
 typedef int v4i_any __attribute__((ext_vector_type(4), aligned(1)));       // (global memory takes 16 bytes at any address)

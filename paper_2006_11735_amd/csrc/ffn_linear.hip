@@ -18,7 +18,7 @@ __device__ __forceinline__ void drain(v4i (&acc)[N])
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(acc[i]));
 }
 
-// One wave a tile of 16 x 16 outputs, operands straight from memory.
+// One wave a tile of 16 x 16 outputs, operands straight from memory: any size, stride and alignment.
 template <bool GATED>
 __global__ __launch_bounds__(256) void linear_plain_kernel(const LinearArgs a, int tiles_n, long long tiles)
 {
@@ -45,10 +45,13 @@ __global__ __launch_bounds__(256) void linear_plain_kernel(const LinearArgs a, i
 
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st)
 {
+    // Up to four rows go token by token (1 x 16384 -> 4096: 12.5 us, by the kernel for few rows 17; 4 rows: 16.3 and 17.2), the others where they take least by what
+    // has been measured; what none of those takes (k below 16, rows gigabytes apart) by the plain kernel.
     const int force = g_tuning.ff_kernel;
-    if (tokens_linear_takes(a) && (force == 7 || force == 0)) return launch_tokens_linear(a, st);
-    if (few_linear_takes(a) && (force == 2 || (force == 0 && a.M <= 64))) return launch_few_linear(a, st);
-    if (tiled_linear_takes(a) && force != 1) return launch_tiled_linear(a, st);
+    const bool few = few_linear_takes(a), tiled = tiled_linear_takes(a);
+    if (tokens_linear_takes(a) && (force == 0 || force == 2)) return launch_tokens_linear(a, st);
+    if (few && (force == 3 || (force == 0 && (!tiled || few_linear_us(a) < tiled_linear_us(a))))) return launch_few_linear(a, st);
+    if (tiled && (force == 0 || force >= 4)) return launch_tiled_linear(a, st);
     const int tiles_n = (a.N + 15) / 16;
     const long long tiles = (long long)((a.M + 15) / 16) * tiles_n, blocks = (tiles + 3) / 4;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;

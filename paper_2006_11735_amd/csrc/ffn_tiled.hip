@@ -406,31 +406,31 @@ struct TileCost {
 };
 constexpr TileCost kTiles[] = {
     {256, 256, 256, 12.f, 1.15f, 1.7f},     // 4096 x 4096 -> 4096: 73 us (the next one: 87); 512 x 4096 -> 4096: 66
-    {128, 128, 512, 6.f, 0.65f, 0.96f},     // gated 512 x 4096 -> 8192: 46 us (the one before 59, the next one 56)
-    {64, 128, 512, 4.f, 0.45f, 0.65f},      // 512 x 4096 -> 4096: 20.6 us (the one before 28.5), 1024 x 4096 -> 4096: 31 us (39 and, by the next one, 41)
-    {64, 64, 512, 3.5f, 0.45f, 0.5f},       // 128 x 4096 -> 4096: 16.8 us (the one before 18.2)
+    {128, 128, 512, 6.f, 0.58f, 0.96f},     // gated 512 x 4096 -> 8192: 46 us (the one before 59, the next one 56)
+    {64, 128, 512, 4.f, 0.29f, 0.65f},      // 512 x 4096 -> 4096: 20.6 us (the one before 28.5), 1024 x 4096 -> 4096: 31 us (39 and, by the next one, 41)
+    {64, 64, 512, 3.5f, 0.25f, 0.5f},       // 128 x 4096 -> 4096: 16.8 us (the one before 18.2)
 };
+
+static float tile_us(const LinearArgs &a, const TileCost &t)
+{
+    const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + t.n - 1) / t.n), turns = __builtin_ceilf(tiles / (float)t.held);
+    const float full = tiles < (float)t.held ? tiles / (float)t.held : 1.f;
+    return turns * (t.fixed + (float)((a.K + 127) / 128) * (t.few + (t.all - t.few) * full));
+}
 
 static int choose_tile(const LinearArgs &a)
 {
     int best = 0;
-    float least = 0.f;
-    for (int c = 0; c < 4; ++c) {
-        const TileCost &t = kTiles[c];
-        const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + t.n - 1) / t.n), turns = __builtin_ceilf(tiles / (float)t.held);
-        const float full = tiles < (float)t.held ? tiles / (float)t.held : 1.f;
-        const float us = turns * (t.fixed + (float)((a.K + 127) / 128) * (t.few + (t.all - t.few) * full));
-        if (c == 0 || us < least) {
-            least = us;
-            best = c;
-        }
-    }
+    for (int c = 1; c < 4; ++c)
+        if (tile_us(a, kTiles[c]) < tile_us(a, kTiles[best])) best = c;
     return best;
 }
 
+float tiled_linear_us(const LinearArgs &a) { return tile_us(a, kTiles[choose_tile(a)]); }
+
 hipError_t launch_tiled_linear(const LinearArgs &a, hipStream_t st)
 {
-    switch (g_tuning.ff_kernel >= 3 ? g_tuning.ff_kernel - 3 : choose_tile(a)) {
+    switch (g_tuning.ff_kernel >= 4 ? g_tuning.ff_kernel - 4 : choose_tile(a)) {
     case 0: return launch_tiles<2, 4, 4, 2, 128, 2>(a, st);
     case 1: return launch_tiles<2, 2, 2, 2, 128, 2>(a, st);
     case 2: return launch_tiles<2, 1, 2, 2, 128, 3>(a, st);

@@ -203,3 +203,26 @@ def test_on_a_stream_of_its_own():
     st = torch.cuda.Stream()
     run(33, 512, 320, "bf16", "silu", gated=True, stream=st)
     run(400, 512, 320, "bf16", residual=True, stream=st)
+
+
+@pytest.fixture
+def kernel():
+    yield lambda k: B.icnn_set_tuning("ff_kernel", k)
+    B.icnn_set_tuning("reset")
+
+
+@pytest.mark.parametrize("which,rows", [(1, 1), (1, 50), (2, 1), (2, 2), (2, 3), (2, 4), (3, 1), (3, 16), (3, 17), (3, 33), (3, 64)] +
+                         [(k, m) for k in (4, 5, 6, 7) for m in (1, 63, 64, 65, 130, 300)])
+@pytest.mark.parametrize("k,n", [(16, 16), (64, 7), (300, 96), (512, 260), (1040, 129), (2320, 520)])
+def test_every_kernel(kernel, which, rows, k, n):
+    kernel(which)
+    for dtype, pads, offset in (("bf16", (0, 0, 0, 0), 0), ("f32", (16, 32, 4, 8), 0), ("f16", (1, 2, 3, 4), 3)):
+        run(rows, k, n, dtype, "gelu", residual=True, pads=pads, offset=offset, seed=which)
+        run(rows, k, n, dtype, "silu", gated=True, pads=pads, offset=offset, seed=which + 10)
+
+
+@pytest.mark.parametrize("k", [1024, 1025, 2047, 2048, 4096, 4111, 8192, 8208, 16384, 16399, 32768, 32780])
+def test_depths_of_single_tokens(k):
+    for rows in (1, 2, 4):
+        run(rows, k, 21, "f32", residual=True, seed=k)
+        run(rows, k, 5, "bf16", "silu", gated=True, seed=k)
