@@ -77,142 +77,113 @@ __global__ __launch_bounds__(256) void rows_kernel(const RowsArgs a)
     }
 }
 
-// Eight numbers of the stream from p[i] on, to and from float32
+// Eight numbers of a stream that is read once
 template <int DT>
-__device__ __forceinline__ void stream_eight(const void *p, long long i, float (&v)[8])
+__device__ __forceinline__ Eight<DT> stream_eight(const void *p, long long i)
 {
-    if (DT == kF32) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const v4f t = __builtin_nontemporal_load((const v4f_any *)((const float *)p + i + 4 * q));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[4 * q + e] = t[e];
-        }
-        return;
+    Eight<DT> r;
+    if constexpr (DT == kF32) {
+        r.b[0] = __builtin_nontemporal_load((const v4i_any *)((const float *)p + i));
+        r.b[1] = __builtin_nontemporal_load((const v4i_any *)((const float *)p + i + 4));
+    } else {
+        r.b[0] = __builtin_nontemporal_load((const v4i_any *)((const uint16_t *)p + i));
     }
-    const v4i t = __builtin_nontemporal_load((const v4i_any *)((const uint16_t *)p + i));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint16_t b = (uint16_t)((uint32_t)t[e >> 1] >> (16 * (e & 1)));
-        v[e] = DT == kF16 ? (float)__builtin_bit_cast(_Float16, b) : __builtin_bit_cast(float, (uint32_t)b << 16);
-    }
-}
-
-// (rounds v as it stores it)
-template <int DT>
-__device__ __forceinline__ v4i pack_eight(float (&v)[8])
-{
-    v4i t;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        uint16_t b[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float &x = v[2 * e + h];
-            b[h] = DT == kF16 ? __builtin_bit_cast(uint16_t, (_Float16)x) : __builtin_bit_cast(uint16_t, (__bf16)x);
-            x = DT == kF16 ? (float)__builtin_bit_cast(_Float16, b[h]) : __builtin_bit_cast(float, (uint32_t)b[h] << 16);
-        }
-        t[e] = (int)(b[0] | (uint32_t)b[1] << 16);
-    }
-    return t;
+    return r;
 }
 
 typedef int v2i_any __attribute__((ext_vector_type(2), aligned(1)));
 
-// Rows that fit a workgroup's registers: read once.  T threads a row (a wave, with neither LDS nor a barrier, or all 256), V times eight numbers a thread.
-template <int DT, int T, int V>
-__global__ __launch_bounds__(256) void rows_held_kernel(const RowsArgs a)
+// Rows that fit a workgroup's registers: read once.  T threads a row (a wave, with neither LDS nor a barrier, or more), V times eight numbers a thread.  All loads of a
+// row are on their way before the first is waited for: they stay bits until then, since a conversion in the branch that has loaded would wait there.
+// DT: the stream's type; GT: gamma's, 0 = no norm.
+template <int DT, int GT, int T, int V>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void rows_held_kernel(const RowsArgs a)
 {
-    const long long row = (long long)blockIdx.x * (256 / T) + threadIdx.x / T;
+    constexpr int WAVES = T / 64, GD = GT ? GT : kF32;
+    const long long row = T < 256 ? (long long)blockIdx.x * (256 / T) + threadIdx.x / T : (long long)blockIdx.x;
     const int t = threadIdx.x % T;
-    if (T == 64 && row >= a.rows) return;
-    float v[V][8], squares = 0.f;
-    uint32_t most = 0;
-    // all loads first
+    if (T < 256 && row >= a.rows) return;
+    Eight<DT> x[V], r[V];
+    Eight<GD> gm[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         const int i = 8 * (k * T + t);
-        if (i + 8 <= a.c) {
-            stream_eight<DT>(a.x, row * a.ldx + i, v[k]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[k][e] = i + e < a.c ? load_number(a.x, row * a.ldx + i + e, DT) : 0.f;
-        }
+        x[k] = {};
+        if (i + 8 <= a.c) x[k] = stream_eight<DT>(a.x, row * a.ldx + i);
+        else if (i < a.c) x[k] = load_up_to_eight<DT>((const uint8_t *)a.x + (row * a.ldx + i) * (DT == kF32 ? 4 : 2), a.c - i);
     }
-    if (a.res) {
-        float u[V][8];
+    if (GT && a.res) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const int i = 8 * (k * T + t);
-            if (i + 8 <= a.c) {
-                stream_eight<DT>(a.res, row * a.ldr + i, u[k]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[k][e] = i + e < a.c ? load_number(a.res, row * a.ldr + i + e, DT) : 0.f;
-            }
+            r[k] = {};
+            if (i + 8 <= a.c) r[k] = stream_eight<DT>(a.res, row * a.ldr + i);
+            else if (i < a.c) r[k] = load_up_to_eight<DT>((const uint8_t *)a.res + (row * a.ldr + i) * (DT == kF32 ? 4 : 2), a.c - i);
         }
-#pragma unroll
-        for (int k = 0; k < V; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[k][e] = round_number(v[k][e] + u[k][e], DT);
     }
-    if (a.sum) {
+    if (GT) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const int i = 8 * (k * T + t);
-            if (i + 8 <= a.c) {
-                if (DT == kF32) {
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-                        *(v4f_any *)((float *)a.sum + row * a.lds + i + 4 * q) = v4f{v[k][4 * q], v[k][4 * q + 1], v[k][4 * q + 2], v[k][4 * q + 3]};
-                } else {
-                    *(v4i_any *)((uint16_t *)a.sum + row * a.lds + i) = pack_eight<DT>(v[k]);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (i + e < a.c) store_number(a.sum, row * a.lds + i + e, DT, v[k][e]);
-            }
+            gm[k] = {};
+            if (i + 8 <= a.c) gm[k] = load_eight<GD>(a.gamma, i);
+            else if (i < a.c) gm[k] = load_up_to_eight<GD>((const uint8_t *)a.gamma + i * (GD == kF32 ? 4 : 2), a.c - i);
         }
     }
-    if (a.gamma) {
+    float v[V][8], squares = 0.f;
+    uint32_t most = 0;
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int i = 8 * (k * T + t);
-            float gm[8];
-            if (i + 8 <= a.c) {
-                if (DT == kF32 || a.gamma_dtype == DT) stream_eight<DT>(a.gamma, i, gm);
-                else stream_eight<kF32>(a.gamma, i, gm);
+    for (int k = 0; k < V; ++k) {
+        const int i = 8 * (k * T + t), left = a.c - i;                     // (numbers behind the row's end repeat its last one: they do not count)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[k][e] = value_of<DT>(x[k], e);
+        if (GT && a.res) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[k][e] = round_number(v[k][e] + value_of<DT>(r[k], e), DT);
+        }
+        if (GT && a.sum) {
+            uint8_t *const at = (uint8_t *)a.sum + (row * a.lds + i) * (DT == kF32 ? 4 : 2);
+            if (left >= 8) {
+                store_eight<DT>(at, 0, v[k]);
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) gm[e] = i + e < a.c ? load_number(a.gamma, i + e, a.gamma_dtype) : 0.f;
+                for (int e = 0; e < 7; ++e)
+                    if (e < left) store_number(at, e, DT, v[k][e]);
             }
+        }
+        if (left < 8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[k][e] = e < left ? v[k][e] : 0.f;
+        }
+        if (GT) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 squares += v[k][e] * v[k][e];
-                v[k][e] *= gm[e];
+                v[k][e] *= value_of<GD>(gm[k], e);
             }
         }
-    }
-#pragma unroll
-    for (int k = 0; k < V; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = max(most, magnitude(v[k][e]));
+    }
 #pragma unroll
     for (int d = 32; d; d >>= 1) {
-        squares += __shfl_xor(squares, d);
+        if (GT) squares += __shfl_xor(squares, d);
         most = max(most, (uint32_t)__shfl_xor((int)most, d));
     }
-    if (T == 256) {
-        __shared__ float squares_of[4];
-        __shared__ uint32_t most_of[4];
+    if constexpr (WAVES > 1) {
+        __shared__ float squares_of[WAVES];
+        __shared__ uint32_t most_of[WAVES];
         if ((t & 63) == 0) {
             squares_of[t >> 6] = squares;
             most_of[t >> 6] = most;
         }
         __syncthreads();
-        squares = (squares_of[0] + squares_of[1]) + (squares_of[2] + squares_of[3]);
-        most = max(max(most_of[0], most_of[1]), max(most_of[2], most_of[3]));
+        squares = 0.f;
+#pragma unroll
+        for (int q = 0; q < WAVES; ++q) {
+            squares += squares_of[q];
+            most = max(most, most_of[q]);
+        }
     }
     float factor, scale;
     row_scale(squares, most, a, &factor, &scale);
@@ -223,35 +194,40 @@ __global__ __launch_bounds__(256) void rows_held_kernel(const RowsArgs a)
         uint32_t b[2] = {};
 #pragma unroll
         for (int e = 0; e < 8; ++e) b[e >> 2] |= (uint32_t)(to_byte(v[k][e], factor) & 255) << (8 * (e & 3));
+        int8_t *const at = a.q + row * a.ldq + i;
         if (i + 8 <= a.c) {
-            *(v2i_any *)(a.q + row * a.ldq + i) = v2i_any{(int)b[0], (int)b[1]};
+            *(v2i_any *)at = v2i_any{(int)b[0], (int)b[1]};
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (i + e < a.c) a.q[row * a.ldq + i + e] = (int8_t)(b[e >> 2] >> (8 * (e & 3)));
+            for (int e = 0; e < 7; ++e)
+                if (i + e < a.c) at[e] = (int8_t)(b[e >> 2] >> (8 * (e & 3)));
         }
     }
 }
 
-template <int DT>
-static void launch_rows_of(const RowsArgs &a, hipStream_t st)
+template <int DT, int GT>
+static hipError_t launch_rows_of(const RowsArgs &a, hipStream_t st)
 {
-    const dim3 waves((unsigned)((a.rows + 3) / 4)), groups((unsigned)a.rows), block(256);
-    if (a.c <= 512) hipLaunchKernelGGL((rows_held_kernel<DT, 64, 1>), waves, block, 0, st, a);
-    else if (a.c <= 1024) hipLaunchKernelGGL((rows_held_kernel<DT, 64, 2>), waves, block, 0, st, a);
-    else if (a.c <= 2048) hipLaunchKernelGGL((rows_held_kernel<DT, 256, 1>), groups, block, 0, st, a);
-    else if (a.c <= 4096) hipLaunchKernelGGL((rows_held_kernel<DT, 256, 2>), groups, block, 0, st, a);
-    else if (a.c <= 8192) hipLaunchKernelGGL((rows_held_kernel<DT, 256, 4>), groups, block, 0, st, a);
-    else if (a.c <= 16384) hipLaunchKernelGGL((rows_held_kernel<DT, 256, 8>), groups, block, 0, st, a);
-    else hipLaunchKernelGGL(rows_kernel, groups, block, 0, st, a);
+    const dim3 four((unsigned)((a.rows + 3) / 4)), one((unsigned)a.rows);
+    if (a.c <= 512) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 64, 1>), four, dim3(256), 0, st, a);
+    else if (a.c <= 1024) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 64, 2>), four, dim3(256), 0, st, a);
+    else if (a.c <= 2048) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 256, 1>), one, dim3(256), 0, st, a);
+    else if (a.c <= 4096) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 256, 2>), one, dim3(256), 0, st, a);
+    else if (a.c <= 6144) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 256, 3>), one, dim3(256), 0, st, a);
+    else if (a.c <= 8192) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 256, 4>), one, dim3(256), 0, st, a);
+    else if (a.c <= 16384) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 1024, 2>), one, dim3(1024), 0, st, a);
+    else if (a.c <= 32768) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 1024, 4>), one, dim3(1024), 0, st, a);
+    else hipLaunchKernelGGL(rows_kernel, one, dim3(256), 0, st, a);
+    return hipGetLastError();
 }
 
 hipError_t launch_rows(const RowsArgs &a, hipStream_t st)
 {
-    if (a.dtype == kF32) launch_rows_of<kF32>(a, st);
-    else if (a.dtype == kF16) launch_rows_of<kF16>(a, st);
-    else launch_rows_of<kBf16>(a, st);
-    return hipGetLastError();
+    const bool f32_gamma = a.gamma_dtype == kF32;
+    if (!a.gamma) return a.dtype == kF32 ? launch_rows_of<kF32, 0>(a, st) : a.dtype == kF16 ? launch_rows_of<kF16, 0>(a, st) : launch_rows_of<kBf16, 0>(a, st);
+    if (a.dtype == kF32) return launch_rows_of<kF32, kF32>(a, st);
+    if (a.dtype == kF16) return f32_gamma ? launch_rows_of<kF16, kF32>(a, st) : launch_rows_of<kF16, kF16>(a, st);
+    return f32_gamma ? launch_rows_of<kBf16, kF32>(a, st) : launch_rows_of<kBf16, kBf16>(a, st);
 }
 
 }  // namespace icnn
