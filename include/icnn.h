@@ -151,6 +151,7 @@ const char *icnn_last_error(void);
  *   "tri_tile"    0 library's choice; 1..4 = the 3x3 + 1x1 + 1x1 kernel at any size, in tiles of 32, 64, 96 or 112 pixels
  *   "ff_kernel"   0 library's choice; products of 8-bit rows, where the shape allows it, by 1 the plain kernel, 2 the one for up to four rows, 3 the one for up to 64
  *                 rows, 4, 5, 6, 7 in tiles of 256 x 256, 128 x 128, 64 x 128, 64 x 64 rows x weight rows
+ *   "ff_split"    0 library's choice; 1 their k axis stays whole; 2..16 it is split into up to so many ranges where the shape and the workspace allow
  *   "ksplit"      0, 1 never split the K axis over workgroups (the library's choice); 2..8 that split where it divides the K steps
  *   "reset"       (value ignored) back to the library's choices
  * Unknown names and values outside these ranges return ICNN_E_PARAM and change nothing. */
@@ -597,8 +598,9 @@ int iquantize_rows_s8(const icnn_norm_desc *desc, const void *x, void *q, float 
  * for every k the descriptor allows and any bytes.  Scales and biases: float32, one per row or output.  y and residual: dtype.  y may not overlap
  * another operand but its residual in place (same pointer and stride): ICNN_E_UNSUPPORTED.
  * workspace: at least ..._workspace_bytes bytes, 16-byte aligned, zero-filled once by the caller after allocating it (its first 4096 bytes are
- * counters that every call leaves at zero); NULL where that is 0.  One workspace of the largest size may serve all calls that run one after the
- * other on a stream; calls that may overlap in time need one each.
+ * counters that every call leaves at zero).  Products of few outputs and a long k want one, for the sums of a k axis that is split over workgroups; others ask for
+ * 0 bytes.  NULL is taken everywhere: k stays whole then, with the same result.  One workspace of the largest size may serve all calls that run one after the other
+ * on a stream; calls that may overlap in time need one each.  The size is that of the tuning in force.
  */
 typedef struct {
     int64_t rows;                  /* 0 <= rows < 2^31                             */

@@ -88,8 +88,21 @@ struct Operand {
     Rows r;
 };
 
+void sizes_of(const icnn_linear_desc *d, LinearArgs &a)
+{
+    a.M = (int)d->rows;
+    a.N = d->n;
+    a.K = d->k;
+    a.ldx = d->x_stride;
+    a.ldw = d->w_stride;
+    a.ldr = d->res_stride;
+    a.ldy = d->y_stride;
+    a.act = d->act;
+    a.dtype = d->dtype;
+}
+
 // Everything behind the descriptor's own check; `a` holds the pointers.
-int run_linear(const icnn_linear_desc *d, LinearArgs &a, const void *workspace, void *stream, const char *what)
+int run_linear(const icnn_linear_desc *d, LinearArgs &a, void *workspace, void *stream, const char *what)
 {
     const int item = item_of(d->dtype);
     if (a.res)
@@ -109,23 +122,19 @@ int run_linear(const icnn_linear_desc *d, LinearArgs &a, const void *workspace, 
         {"residual", a.res, rows_of(a.res, d->rows, d->res_stride, d->n, item)}};
     for (const Operand &o : in)
         if (o.p && share(y, o.r) && !(o.p == a.res && same(y, o.r))) return fail(ICNN_E_UNSUPPORTED, "y overlaps %s", o.name);
-    a.M = (int)d->rows;
-    a.N = d->n;
-    a.K = d->k;
-    a.ldx = d->x_stride;
-    a.ldw = d->w_stride;
-    a.ldr = d->res_stride;
-    a.ldy = d->y_stride;
-    a.act = d->act;
-    a.dtype = d->dtype;
+    sizes_of(d, a);
+    a.workspace = workspace;
     return launched(launch_linear(a, (hipStream_t)stream), what);
 }
 
-int workspace_bytes(const icnn_linear_desc *desc, size_t *bytes)
+int workspace_bytes(const icnn_linear_desc *desc, bool gated, size_t *bytes)
 {
     if (int rc = check_linear(desc)) return rc;
     if (!bytes) return fail(ICNN_E_NULL, "bytes is NULL");
-    *bytes = 0;
+    LinearArgs a = {};
+    sizes_of(desc, a);
+    a.w2 = gated ? (const int8_t *)16 : nullptr;           // (whether there is one; never read)
+    *bytes = desc->rows ? linear_workspace(a) : 0;
     return ICNN_OK;
 }
 
@@ -182,9 +191,9 @@ int iquantize_rows_s8(const icnn_norm_desc *d, const void *x, void *q, float *sc
     return launched(launch_rows(a, (hipStream_t)stream), "iquantize_rows_s8");
 }
 
-int ilinear_s8_workspace_bytes(const icnn_linear_desc *desc, size_t *bytes) { return workspace_bytes(desc, bytes); }
+int ilinear_s8_workspace_bytes(const icnn_linear_desc *desc, size_t *bytes) { return workspace_bytes(desc, false, bytes); }
 
-int igated_linear_s8_workspace_bytes(const icnn_linear_desc *desc, size_t *bytes) { return workspace_bytes(desc, bytes); }
+int igated_linear_s8_workspace_bytes(const icnn_linear_desc *desc, size_t *bytes) { return workspace_bytes(desc, true, bytes); }
 
 int ilinear_s8(const icnn_linear_desc *desc, const void *x, const float *x_scale, const void *w, const float *w_scale, const float *bias,
                const void *residual, void *y, void *workspace, void *stream)

@@ -23,6 +23,7 @@ struct LinearArgs {
     const float *xs, *ws, *ws2, *bias, *bias2;
     const void *res;
     void *y;
+    void *workspace;                // null: k stays whole
     long long ldx, ldw, ldr, ldy;
     int M, N, K;
     int act, dtype;
@@ -30,6 +31,7 @@ struct LinearArgs {
 
 hipError_t launch_rows(const RowsArgs &a, hipStream_t st);
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st);
+size_t linear_workspace(const LinearArgs &a);
 // kernels of ffn_tokens.hip, ffn_few.hip and ffn_tiled.hip: whether they take a product's shape, and about how long it takes them
 bool tokens_linear_takes(const LinearArgs &a);
 hipError_t launch_tokens_linear(const LinearArgs &a, hipStream_t st);
@@ -37,7 +39,8 @@ bool few_linear_takes(const LinearArgs &a);
 float few_linear_us(const LinearArgs &a);
 hipError_t launch_few_linear(const LinearArgs &a, hipStream_t st);
 bool tiled_linear_takes(const LinearArgs &a);
-float tiled_linear_us(const LinearArgs &a);
+float tiled_linear_us(const LinearArgs &a, bool may_split);
+size_t tiled_linear_workspace(const LinearArgs &a);      // of counters and partial sums
 hipError_t launch_tiled_linear(const LinearArgs &a, hipStream_t st);
 
 typedef int v4i_any __attribute__((ext_vector_type(4), aligned(1)));       // (global memory takes 16 bytes at any address)

@@ -20,6 +20,11 @@ typedef __attribute__((address_space(3))) void LdsVoid;
 struct TiledArgs {
     LinearArgs l;
     int tiles_n, tiles_m, per_xcd;
+    // Split k: a tile's steps in `splits` ranges of `steps_per` (the last one may have fewer), each a workgroup of its own.  A range leaves its sums in `part`; the
+    // one that arrives last at the tile's counter adds the others' and finishes the tile.  The sums are integers: the order of arrival changes nothing.
+    int splits, steps_per;
+    int32_t *part;
+    unsigned *counters;            // zero before the launch and after it
 };
 
 // Row q's 16-byte piece c lies at c ^ piece_key(q) in its stage.  LDS hands out 256 bytes at a time, the pieces of sixteen lanes: those read the same piece of sixteen
@@ -69,8 +74,9 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
     static_assert(LW * ROWS * NW == BN && LX * ROWS * NW == BM && SLICES >= 2 && SLICES % 2 == 0, "whole copies, two fragment sets in turn");
     extern __shared__ __align__(1024) uint8_t lds[];
     const LinearArgs &a = ta.l;
-    const int slot = (int)(blockIdx.x & 7) * ta.per_xcd + (int)(blockIdx.x >> 3);
-    if (slot >= ta.tiles_n * ta.tiles_m) return;
+    const int unit = (int)(blockIdx.x & 7) * ta.per_xcd + (int)(blockIdx.x >> 3);
+    if (unit >= ta.tiles_n * ta.tiles_m * ta.splits) return;
+    const int slot = unit / ta.splits, range = unit - slot * ta.splits;
     // eight rows of tiles, column after column: what an XCD has at one time shares its weights and rows
     constexpr int GROUP = 8;
     const int panel = slot / (GROUP * ta.tiles_n), in_panel = slot - panel * GROUP * ta.tiles_n, high = min(GROUP, ta.tiles_m - panel * GROUP);
@@ -100,11 +106,11 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
         piece_x[j] = (lane % PIECES) ^ piece_key<BK, false>(q);
         off_x[j] = (unsigned)min(q, a.M - 1 - m0) * (unsigned)a.ldx + 16 * piece_x[j];
     }
-    const int steps = (a.K + BK - 1) / BK;
+    const int first = range * ta.steps_per * BK, steps = min(ta.steps_per, (a.K - first + BK - 1) / BK), end = min(a.K, first + steps * BK);
     // copies FROM .. TO - 1 of step s: of the weights, then of the rows.  Behind the last step nothing but zeros comes.
     auto copy_part = [&](int s, auto from, auto to) {
         uint8_t *const at = lds + (s % STAGES) * STAGE + wave * 1024;
-        const int k0 = s * BK, left = a.K - k0;
+        const int k0 = first + s * BK, left = end - k0;
 #pragma unroll
         for (int j = from; j < to; ++j) {
             if (j < LW) {
@@ -119,7 +125,7 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
     // The same through registers, for rows that start anywhere: fetch_step's loads are in flight while a stage is multiplied, put_step's stores follow
     v4i held[LOADS];
     auto fetch_step = [&](int s) {
-        const int k0 = s * BK;
+        const int k0 = first + s * BK;
         const int8_t *const w0 = a.w + n0 * a.ldw + k0, *const w1 = (GATED ? a.w2 : a.w) + n0 * a.ldw + k0, *const x0 = a.x + m0 * a.ldx + k0;
         if (k0 + BK <= a.K) {
 #pragma unroll
@@ -227,6 +233,54 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
     }
     FFN_WAIT_VMCNT(0);
     drain(acc);
+
+    if (ta.splits > 1) {
+        // The partial sums are written through to memory and read past the caches (16: a scope of the whole chip), so they are coherent between the XCDs' L2
+        // caches; a store has reached memory when the wave's counter of outstanding operations says so.  No workgroup waits for another.
+        constexpr unsigned UNIT = NW * 64 * TN * TM * 64;
+        const __amdgpu_buffer_rsrc_t rs_part = __builtin_amdgcn_make_buffer_rsrc((void *)ta.part, 0, 0x7fffffff, 0x20000);
+        const unsigned mine = (unsigned)unit * UNIT + threadIdx.x * 16;
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int j = 0; j < TM; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    __builtin_amdgcn_raw_buffer_store_b128(v4i{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]}, rs_part,
+                                                           mine + ((i * TM + j) * 4 + e) * (NW * 1024), 0, 16);
+        asm volatile("" ::: "memory");
+        FFN_WAIT_VMCNT(0);
+        __syncthreads();                                   // every wave's sums are in memory, and LDS is free
+        if (threadIdx.x == 0) {
+            const bool last = atomicAdd(ta.counters + slot, 1u) == (unsigned)ta.splits - 1;
+            if (last) ta.counters[slot] = 0;               // all have arrived: ready for the next call
+            *(int *)lds = last;
+        }
+        __syncthreads();
+        if (!*(const int *)lds) return;
+        constexpr int AT_ONCE = TN * TM <= 2 ? 4 : 1;      // ranges whose sums are on their way together
+        for (int o = 1; o < ta.splits; o += AT_ONCE) {
+            v4i t[AT_ONCE][TN * TM * 4];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                if (o + u >= ta.splits) continue;
+                const int other = range + o + u < ta.splits ? range + o + u : range + o + u - ta.splits;
+                const unsigned theirs = (unsigned)(slot * ta.splits + other) * UNIT + threadIdx.x * 16;
+#pragma unroll
+                for (int g = 0; g < TN * TM * 4; ++g) t[u][g] = __builtin_amdgcn_raw_buffer_load_b128(rs_part, theirs + g * (NW * 1024), 0, 16);
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                if (o + u >= ta.splits) continue;
+#pragma unroll
+                for (int g = 0; g < TN * TM * 4; ++g) {
+                    v16i &c = acc[g / 4 / TM][g / 4 % TM];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) c[4 * (g & 3) + e] += t[u][g][e];
+                }
+            }
+        }
+    }
 
     // ---- epilogue.  The sums go through LDS (as many of the tile's rows at a time as fit) into an order in which a thread has eight outputs n next to each
     // other of row after row: it reads their scales and biases once, a row's residual and y are read and written in whole lines, and the loads of several rows are in
@@ -374,15 +428,20 @@ static bool direct(const LinearArgs &a)
 }
 
 template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED, bool DIRECT>
-static hipError_t launch_one(const LinearArgs &a, hipStream_t st)
+static hipError_t launch_one(const LinearArgs &a, int splits, hipStream_t st)
 {
     constexpr int BN = 32 * TN * WN / (GATED ? 2 : 1), BM = 32 * TM * WM, LDS = 32 * (TN * WN + TM * WM) * BK * STAGES;
     TiledArgs t;
     t.l = a;
     t.tiles_n = (a.N + BN - 1) / BN;
     t.tiles_m = (a.M + BM - 1) / BM;
-    const long long tiles = (long long)t.tiles_n * t.tiles_m, per = (tiles + 7) / 8;
-    if (tiles > 0x7ffffff0LL) return hipErrorInvalidValue;
+    const int steps = (a.K + BK - 1) / BK;
+    t.steps_per = (steps + splits - 1) / splits;
+    t.splits = (steps + t.steps_per - 1) / t.steps_per;    // (no range without a step)
+    t.counters = (unsigned *)a.workspace;
+    t.part = (int32_t *)((uint8_t *)a.workspace + kWsCounterBytes);
+    const long long units = (long long)t.tiles_n * t.tiles_m * t.splits, per = (units + 7) / 8;
+    if (units > 0x7ffffff0LL) return hipErrorInvalidValue;
     t.per_xcd = (int)per;
     auto *const k = linear_tiled_kernel<TN, TM, WN, WM, BK, STAGES, GATED, DIRECT>;
     if (LDS > 65536)
@@ -392,14 +451,16 @@ static hipError_t launch_one(const LinearArgs &a, hipStream_t st)
 }
 
 template <int TN, int TM, int WN, int WM, int BK, int STAGES>
-static hipError_t launch_tiles(const LinearArgs &a, hipStream_t st)
+static hipError_t launch_tiles(const LinearArgs &a, int splits, hipStream_t st)
 {
-    if (direct(a)) return a.w2 ? launch_one<TN, TM, WN, WM, BK, STAGES, true, true>(a, st) : launch_one<TN, TM, WN, WM, BK, STAGES, false, true>(a, st);
-    return a.w2 ? launch_one<TN, TM, WN, WM, 128, 2, true, false>(a, st) : launch_one<TN, TM, WN, WM, 128, 2, false, false>(a, st);
+    if (direct(a))
+        return a.w2 ? launch_one<TN, TM, WN, WM, BK, STAGES, true, true>(a, splits, st) : launch_one<TN, TM, WN, WM, BK, STAGES, false, true>(a, splits, st);
+    return a.w2 ? launch_one<TN, TM, WN, WM, BK, 2, true, false>(a, splits, st) : launch_one<TN, TM, WN, WM, BK, 2, false, false>(a, splits, st);
 }
 
-// Which tile.  A tile's time is a part that does not depend on k (start, epilogue) and one for each 128 bytes of k; tiles beyond what the 256 compute units
-// hold at a time wait for another turn.  Measured in us: {rows, weight rows, held at a time, fixed, a step with few tiles on the chip, a step with all}.
+// Which tile, and in how many ranges of k.  A tile's time is a part that does not depend on k (start, epilogue) and one for each 128 bytes of k; tiles beyond what
+// the 256 compute units hold at a time wait for another turn.  Measured in us: {rows, weight rows, held at a time, fixed, a step with few tiles on the chip, a
+// step with all}.
 struct TileCost {
     int m, n, held;
     float fixed, few, all;
@@ -410,31 +471,51 @@ constexpr TileCost kTiles[] = {
     {64, 128, 512, 4.f, 0.29f, 0.65f},      // 512 x 4096 -> 4096: 20.6 us (the one before 28.5), 1024 x 4096 -> 4096: 31 us (39 and, by the next one, 41)
     {64, 64, 512, 3.5f, 0.25f, 0.5f},       // 128 x 4096 -> 4096: 16.8 us (the one before 18.2)
 };
+constexpr int kMostSplits = 16, kSplitTiles = (int)(kWsCounterBytes / sizeof(unsigned));
+constexpr float kExchange = 1.f, kExchangeRange = 0.6f;        // us: the sums' way through memory, and so much more for each range to add
 
-static float tile_us(const LinearArgs &a, const TileCost &t)
-{
-    const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + t.n - 1) / t.n), turns = __builtin_ceilf(tiles / (float)t.held);
-    const float full = tiles < (float)t.held ? tiles / (float)t.held : 1.f;
-    return turns * (t.fixed + (float)((a.K + 127) / 128) * (t.few + (t.all - t.few) * full));
-}
+struct TilePlan {
+    int tile, splits;
+    float us;
+};
 
-static int choose_tile(const LinearArgs &a)
+static TilePlan plan_tiles(const LinearArgs &a, bool may_split)
 {
-    int best = 0;
-    for (int c = 1; c < 4; ++c)
-        if (tile_us(a, kTiles[c]) < tile_us(a, kTiles[best])) best = c;
+    TilePlan best = {0, 1, 0.f};
+    const int steps = (a.K + 127) / 128;
+    for (int c = 0; c < 4; ++c) {
+        if (g_tuning.ff_kernel >= 4 && c != g_tuning.ff_kernel - 4) continue;
+        const TileCost &t = kTiles[c];
+        const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + t.n - 1) / t.n);
+        for (int s = 1; s <= kMostSplits; ++s) {
+            if (s > 1 && (!may_split || tiles > (float)kSplitTiles || tiles * (float)s > (float)t.held || 2 * s > steps)) break;
+            const float units = tiles * (float)s, turns = __builtin_ceilf(units / (float)t.held), full = units < (float)t.held ? units / (float)t.held : 1.f;
+            const float us = turns * (t.fixed + (float)((steps + s - 1) / s) * (t.few + (t.all - t.few) * full)) + (s > 1 ? kExchange + kExchangeRange * (float)s : 0.f);
+            if (g_tuning.ff_split ? s == 1 || s <= g_tuning.ff_split : best.us == 0.f || us < best.us) best = {c, s, us};
+        }
+    }
     return best;
 }
 
-float tiled_linear_us(const LinearArgs &a) { return tile_us(a, kTiles[choose_tile(a)]); }
+float tiled_linear_us(const LinearArgs &a, bool may_split) { return plan_tiles(a, may_split).us; }
+
+size_t tiled_linear_workspace(const LinearArgs &a)
+{
+    const TilePlan p = plan_tiles(a, true);
+    if (p.splits == 1) return 0;
+    const TileCost &t = kTiles[p.tile];
+    const size_t tiles = (size_t)((a.M + t.m - 1) / t.m) * (size_t)(((a.w2 ? 2ll : 1ll) * a.N + t.n - 1) / t.n);
+    return kWsCounterBytes + tiles * (size_t)p.splits * (size_t)(t.m * t.n) * 4;
+}
 
 hipError_t launch_tiled_linear(const LinearArgs &a, hipStream_t st)
 {
-    switch (g_tuning.ff_kernel >= 4 ? g_tuning.ff_kernel - 4 : choose_tile(a)) {
-    case 0: return launch_tiles<2, 4, 4, 2, 128, 2>(a, st);
-    case 1: return launch_tiles<2, 2, 2, 2, 128, 2>(a, st);
-    case 2: return launch_tiles<2, 1, 2, 2, 128, 3>(a, st);
-    default: return launch_tiles<2, 1, 1, 2, 128, 4>(a, st);
+    const TilePlan p = plan_tiles(a, a.workspace != nullptr);
+    switch (p.tile) {
+    case 0: return launch_tiles<2, 4, 4, 2, 128, 2>(a, p.splits, st);
+    case 1: return launch_tiles<2, 2, 2, 2, 128, 2>(a, p.splits, st);
+    case 2: return launch_tiles<2, 1, 2, 2, 128, 3>(a, p.splits, st);
+    default: return launch_tiles<2, 1, 1, 2, 128, 4>(a, p.splits, st);
     }
 }
 

@@ -226,3 +226,78 @@ def test_depths_of_single_tokens(k):
     for rows in (1, 2, 4):
         run(rows, k, 21, "f32", residual=True, seed=k)
         run(rows, k, 5, "bf16", "silu", gated=True, seed=k)
+
+
+@pytest.fixture
+def split():
+    yield lambda kernel, ranges: (B.icnn_set_tuning("ff_kernel", kernel), B.icnn_set_tuning("ff_split", ranges))
+    B.icnn_set_tuning("reset")
+
+
+@pytest.mark.parametrize("which", [4, 5, 6, 7])
+@pytest.mark.parametrize("ranges", [2, 3, 7, 16])
+@pytest.mark.parametrize("rows,k,n", [(7, 640, 40), (70, 2048, 200), (150, 4104, 130), (300, 1001, 90)])
+def test_split_k(split, which, ranges, rows, k, n):
+    split(which, ranges)
+    for gated in (False, True):
+        size = (B.igated_linear_s8_workspace_bytes if gated else B.ilinear_s8_workspace_bytes)(B.linear_desc(rows=rows, k=k, n=n))
+        assert size > 4096
+        run(rows, k, n, "f32", "silu" if gated else "none", gated=gated, residual=not gated, seed=ranges)
+        run(rows, k, n, "bf16", "gelu", gated=gated, residual=not gated, pads=(3, 5, 2, 1), offset=1, seed=ranges)
+
+
+def test_every_kernel_gives_the_same_bits_with_and_without_a_workspace():
+    rows, k, n = 33, 4096, 320
+    g = np.random.default_rng(9)
+    dev = lambda v: torch.from_numpy(v).to("cuda:0")  # noqa: E731
+    x, (w, ws), (w2, ws2) = dev(g.integers(-127, 128, size=(rows, k)).astype(np.int8)), *[tuple(dev(v) for v in weights(g, n, k, False)) for _ in range(2)]
+    xs, b, res = dev(g.uniform(0.5, 1.5, size=rows).astype(np.float32) / 40), dev(g.normal(size=n).astype(np.float32)), dev(g.normal(size=(rows, n)).astype(np.float32))
+    d = B.linear_desc(rows=rows, k=k, n=n, act=B.ICNN_ACT_GELU_TANH, dtype=B.ICNN_F32)
+    first = None
+    try:
+        for which in (0, 1, 3, 4, 5, 6, 7):
+            for ranges in (0, 1, 5):
+                B.icnn_set_tuning("ff_kernel", which)
+                B.icnn_set_tuning("ff_split", ranges)
+                for gated in (False, True):
+                    size = (B.igated_linear_s8_workspace_bytes if gated else B.ilinear_s8_workspace_bytes)(d)
+                    space = torch.zeros(max(size, 4096), dtype=torch.uint8, device="cuda:0")
+                    outs = []
+                    for s in (space if size else None, None):
+                        y = torch.empty((rows, n), device="cuda:0")
+                        if gated:
+                            B.igated_linear_s8(d, x, xs, w, ws, b, w2, ws2, None, y, s)
+                        else:
+                            B.ilinear_s8(d, x, xs, w, ws, b, res, y, s)
+                        outs.append(y)
+                    torch.cuda.synchronize()
+                    assert torch.equal(outs[0], outs[1])
+                    first = first or {}
+                    assert torch.equal(first.setdefault(gated, outs[0]), outs[0]), (which, ranges, gated)
+    finally:
+        B.icnn_set_tuning("reset")
+
+
+def test_a_graph_replays_with_a_workspace():
+    """Split k on one workspace, call after call, replayed: every replay against the eager result."""
+    rows, k, n = 40, 16384, 256
+    g = np.random.default_rng(10)
+    dev = lambda v: torch.from_numpy(v).to("cuda:0")  # noqa: E731
+    w, ws = (dev(v) for v in weights(g, n, k, False))
+    x, xs = torch.zeros((rows, k), dtype=torch.int8, device="cuda:0"), dev(g.uniform(0.5, 1.5, size=rows).astype(np.float32) / 40)
+    d = B.linear_desc(rows=rows, k=k, n=n, dtype=B.ICNN_F32)
+    size = B.ilinear_s8_workspace_bytes(d)
+    assert size > 4096
+    space, y, eager = torch.zeros(size, dtype=torch.uint8, device="cuda:0"), torch.empty((rows, n), device="cuda:0"), torch.empty((rows, n), device="cuda:0")
+    B.ilinear_s8(d, x, xs, w, ws, None, None, y, space)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(3):
+            B.ilinear_s8(d, x, xs, w, ws, None, None, y, space)
+    for k_ in range(5):
+        x.copy_(dev(g.integers(-127, 128, size=(rows, k)).astype(np.int8)))
+        B.ilinear_s8(d, x, xs, w, ws, None, None, eager)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, eager) and not space[:4096].any(), k_
