@@ -130,3 +130,24 @@ def test_lists_of_calls_refuse_as_the_calls_do():
     with pytest.raises(B.IcnnError) as e:
         B._check(B._lib.icnn_run_calls(1, ctypes.byref(missing), 0))
     assert e.value.code == B.ICNN_E_NULL
+
+
+def test_a_block_refuses_shapes_that_do_not_fit():
+    from paper_2006_11735_amd.ffn import FeedForward
+    z = torch.zeros
+    good = dict(gamma=z(8), w_gate=z(16, 8), w_up=z(16, 8), w_down=z(8, 16), rows=4)
+    for kw in (dict(gamma=z(9)), dict(w_up=z(16, 9)), dict(w_down=z(16, 8)), dict(b_gate=z(8)), dict(b_down=z(16)), dict(w_up=None, b_up=z(16)), dict(act="tanh"),
+               dict(dtype=torch.float64), dict(rows=0)):
+        with pytest.raises(ValueError):
+            FeedForward(**{**good, **kw})
+
+
+def test_workspaces_are_asked_for_where_k_is_long_and_outputs_are_few():
+    size = lambda **kw: B.ilinear_s8_workspace_bytes(B.linear_desc(**kw))  # noqa: E731
+    assert size(rows=64, k=16384, n=512) > 4096 and size(rows=1, k=16384, n=512) == 0 and size(rows=4096, k=16384, n=4096) == 0
+    assert size(rows=64, k=256, n=512) == 0 and size(rows=0, k=16384, n=512) == 0
+    try:
+        B.icnn_set_tuning("ff_split", 1)
+        assert size(rows=64, k=16384, n=512) == 0
+    finally:
+        B.icnn_set_tuning("reset")
