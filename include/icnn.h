@@ -150,7 +150,7 @@ const char *icnn_last_error(void);
  *   "flat"        0 library's choice; 1 / 2: every / no layer whose shape it takes on the kernel that streams weights into registers
  *   "tri_tile"    0 library's choice; 1..4 = the 3x3 + 1x1 + 1x1 kernel at any size, in tiles of 32, 64, 96 or 112 pixels
  *   "ff_kernel"   0 library's choice; products of 8-bit rows, where the shape allows it, by 1 the plain kernel, 2 the one for up to four rows, 3 the one for up to 64
- *                 rows, 4, 5, 6, 7 in tiles of 256 x 256, 128 x 128, 64 x 128, 64 x 64 rows x weight rows
+ *                 rows, 4..9 in tiles of 256 x 256, 128 x 256, 128 x 128 (two or one on a compute unit), 64 x 128, 64 x 64 rows x weight rows
  *   "ff_split"    0 library's choice; 1 their k axis stays whole; 2..16 it is split into up to so many ranges where the shape and the workspace allow
  *   "ksplit"      0, 1 never split the K axis over workgroups (the library's choice); 2..8 that split where it divides the K steps
  *   "reset"       (value ignored) back to the library's choices

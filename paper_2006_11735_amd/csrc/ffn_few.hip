@@ -182,7 +182,7 @@ bool few_linear_takes(const LinearArgs &a) { return a.M <= 64 && a.K >= 16 && a.
 float few_linear_us(const LinearArgs &a)
 {
     const float mb = (a.w2 ? 2.f : 1.f) * (float)a.N * (float)a.K * 1e-6f, turns = (float)((a.K + NW * RB - 1) / (NW * RB));
-    const float flow = a.M <= 16 ? 3.2f + 0.2f * mb : a.M <= 32 ? 5.f + 0.215f * mb : 5.f + 0.5f * mb;
+    const float flow = a.M <= 16 ? 3.2f + 0.2f * mb : a.M <= 32 ? 5.f + 0.215f * mb : 6.5f + 0.47f * mb;
     const float chain = 3.f + turns * (a.M <= 16 ? 0.8f : a.M <= 32 ? 0.85f : 2.f);
     return flow > chain ? flow : chain;
 }

@@ -466,13 +466,18 @@ struct TileCost {
     float fixed, few, all;
 };
 constexpr TileCost kTiles[] = {
-    {256, 256, 256, 12.f, 1.15f, 1.7f},     // 4096 x 4096 -> 4096: 73 us (the next one: 87); 512 x 4096 -> 4096: 66
-    {128, 128, 512, 6.f, 0.58f, 0.96f},     // gated 512 x 4096 -> 8192: 46 us (the one before 59, the next one 56)
-    {64, 128, 512, 4.f, 0.29f, 0.65f},      // 512 x 4096 -> 4096: 20.6 us (the one before 28.5), 1024 x 4096 -> 4096: 31 us (39 and, by the next one, 41)
-    {64, 64, 512, 3.5f, 0.25f, 0.5f},       // 128 x 4096 -> 4096: 16.8 us (the one before 18.2)
+    {256, 256, 256, 14.f, 1.15f, 1.75f},    // 4096 x 4096 -> 4096: 74 us (the next one: 79)
+    {128, 256, 256, 8.f, 0.55f, 1.f},       // gated 512 x 4096 -> 8192: 40 us (the one before 59, the next one 45)
+    {128, 128, 512, 6.f, 0.58f, 1.25f},     // two workgroups on a compute unit
+    {128, 128, 256, 8.5f, 0.48f, 0.58f},    // ... one, with four stages instead of two: 1024 x 4096 -> 4096: 26 us (the one before 35, the next one 30)
+    {64, 128, 512, 4.f, 0.29f, 0.75f},      // gated 77 x 2048 -> 5461: 9.4 us (the next one 10.2)
+    {64, 64, 512, 3.f, 0.22f, 0.46f},       // 128 x 4096 -> 4096: 10.2 us (the one before 13.9), 512 x 4096 -> 4096: 16.4 us (16.3)
 };
+constexpr int kTileKinds = sizeof(kTiles) / sizeof(kTiles[0]);
 constexpr int kMostSplits = 16, kSplitTiles = (int)(kWsCounterBytes / sizeof(unsigned));
-constexpr float kExchange = 1.f, kExchangeRange = 0.6f;        // us: the sums' way through memory, and so much more for each range to add
+// us: the sums' way through memory and back, so much more for each range that one workgroup adds, and for each 64 x 64 sums that take it (64 x 16384 -> 512 in 64 x 64
+// tiles: whole 35 us, in 2, 4, 8, 16 ranges 20.9, 14.4, 12.6, 15.1; 512 x 4096 -> 4096 in two ranges of 64 x 128 tiles 23.8, whole 16.3)
+constexpr float kExchange = 0.5f, kExchangeRange = 0.55f, kExchangeSums = 0.006f;
 
 struct TilePlan {
     int tile, splits;
@@ -483,14 +488,14 @@ static TilePlan plan_tiles(const LinearArgs &a, bool may_split)
 {
     TilePlan best = {0, 1, 0.f};
     const int steps = (a.K + 127) / 128;
-    for (int c = 0; c < 4; ++c) {
+    for (int c = 0; c < kTileKinds; ++c) {
         if (g_tuning.ff_kernel >= 4 && c != g_tuning.ff_kernel - 4) continue;
         const TileCost &t = kTiles[c];
         const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + t.n - 1) / t.n);
         for (int s = 1; s <= kMostSplits; ++s) {
             if (s > 1 && (!may_split || tiles > (float)kSplitTiles || tiles * (float)s > (float)t.held || 2 * s > steps)) break;
             const float units = tiles * (float)s, turns = __builtin_ceilf(units / (float)t.held), full = units < (float)t.held ? units / (float)t.held : 1.f;
-            const float us = turns * (t.fixed + (float)((steps + s - 1) / s) * (t.few + (t.all - t.few) * full)) + (s > 1 ? kExchange + kExchangeRange * (float)s : 0.f);
+            const float us = turns * (t.fixed + (float)((steps + s - 1) / s) * (t.few + (t.all - t.few) * full)) + (s > 1 ? kExchange + kExchangeRange * (float)s + kExchangeSums * units * (float)(t.m * t.n / 4096) : 0.f);
             if (g_tuning.ff_split ? s == 1 || s <= g_tuning.ff_split : best.us == 0.f || us < best.us) best = {c, s, us};
         }
     }
@@ -513,9 +518,13 @@ hipError_t launch_tiled_linear(const LinearArgs &a, hipStream_t st)
     const TilePlan p = plan_tiles(a, a.workspace != nullptr);
     switch (p.tile) {
     case 0: return launch_tiles<2, 4, 4, 2, 128, 2>(a, p.splits, st);
-    case 1: return launch_tiles<2, 2, 2, 2, 128, 2>(a, p.splits, st);
-    case 2: return launch_tiles<2, 1, 2, 2, 128, 3>(a, p.splits, st);
-    default: return launch_tiles<2, 1, 1, 2, 128, 4>(a, p.splits, st);
+    case 1: return launch_tiles<2, 2, 4, 2, 128, 3>(a, p.splits, st);
+    case 2: return launch_tiles<2, 2, 2, 2, 128, 2>(a, p.splits, st);
+    case 3: return launch_tiles<2, 2, 2, 2, 128, 4>(a, p.splits, st);
+    case 4: return launch_tiles<2, 1, 2, 2, 128, 3>(a, p.splits, st);
+    default:                                               // (four waves where gate and up need not be in one: 24 x 256 -> 8192 3.6 us, by two waves 4.2)
+        if (a.w2) return launch_tiles<2, 1, 1, 2, 128, 4>(a, p.splits, st);
+        return direct(a) ? launch_one<1, 1, 2, 2, 128, 4, false, true>(a, p.splits, st) : launch_one<1, 1, 2, 2, 128, 2, false, false>(a, p.splits, st);
     }
 }
 

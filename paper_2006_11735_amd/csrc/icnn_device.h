@@ -263,7 +263,7 @@ struct Tuning {
     int keep = 0;          // 3x3 layers of 64 channels with their weights kept in registers: 1 every layer that kernel accepts, 2 none
     int flat = 0;          // kernel with register-fed weights: 1 every layer whose shape it accepts, 2 none
     int tri_tile = 0;      // 3x3 + 1x1 + 1x1 kernel: 1..4 = tiles of 32, 64, 96 or 112 pixels
-    int ff_kernel = 0;     // products of 8-bit rows: 1 plain kernel, 2 token by token, 3 few rows, 4..7 a tile size, where the shape allows
+    int ff_kernel = 0;     // products of 8-bit rows: 1 plain kernel, 2 token by token, 3 few rows, 4..9 a tile size, where the shape allows
     int ff_split = 0;      // their k axis in tiles: 1 whole, 2..16 in up to so many ranges
     int ksplit = 0;        // 0, 1 the K axis stays whole (the library's choice); 2..8 this split where it divides the K steps
 };

@@ -212,7 +212,7 @@ def kernel():
 
 
 @pytest.mark.parametrize("which,rows", [(1, 1), (1, 50), (2, 1), (2, 2), (2, 3), (2, 4), (3, 1), (3, 16), (3, 17), (3, 33), (3, 64)] +
-                         [(k, m) for k in (4, 5, 6, 7) for m in (1, 63, 64, 65, 130, 300)])
+                         [(k, m) for k in range(4, 10) for m in (1, 63, 64, 65, 130, 300)])
 @pytest.mark.parametrize("k,n", [(16, 16), (64, 7), (300, 96), (512, 260), (1040, 129), (2320, 520)])
 def test_every_kernel(kernel, which, rows, k, n):
     kernel(which)
@@ -234,7 +234,7 @@ def split():
     B.icnn_set_tuning("reset")
 
 
-@pytest.mark.parametrize("which", [4, 5, 6, 7])
+@pytest.mark.parametrize("which", range(4, 10))
 @pytest.mark.parametrize("ranges", [2, 3, 7, 16])
 @pytest.mark.parametrize("rows,k,n", [(7, 640, 40), (70, 2048, 200), (150, 4104, 130), (300, 1001, 90)])
 def test_split_k(split, which, ranges, rows, k, n):
@@ -255,7 +255,7 @@ def test_every_kernel_gives_the_same_bits_with_and_without_a_workspace():
     d = B.linear_desc(rows=rows, k=k, n=n, act=B.ICNN_ACT_GELU_TANH, dtype=B.ICNN_F32)
     first = None
     try:
-        for which in (0, 1, 3, 4, 5, 6, 7):
+        for which in (0, 1, 3, 4, 5, 6, 7, 8, 9):
             for ranges in (0, 1, 5):
                 B.icnn_set_tuning("ff_kernel", which)
                 B.icnn_set_tuning("ff_split", ranges)
