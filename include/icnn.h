@@ -577,7 +577,7 @@ typedef enum {
  * another output: ICNN_E_UNSUPPORTED.  iquantize_rows_s8 uses rows, c, x_stride, q_stride and dtype.
  */
 typedef struct {
-    int64_t rows;                  /* 0 <= rows < 2^31                             */
+    int64_t rows;                  /* 0 <= rows <= 2^31 - 2^16                     */
     int64_t x_stride, res_stride, sum_stride, q_stride;   /* c <= stride <= 2^40, rows * stride <= 2^44 */
     int32_t c;                     /* 1 <= c <= 2^20                               */
     int32_t dtype;                 /* of x, residual and sum: ICNN_F32, F16 or BF16 */
@@ -603,10 +603,10 @@ int iquantize_rows_s8(const icnn_norm_desc *desc, const void *x, void *q, float 
  * on a stream; calls that may overlap in time need one each.  The size is that of the tuning in force.
  */
 typedef struct {
-    int64_t rows;                  /* 0 <= rows < 2^31                             */
+    int64_t rows;                  /* 0 <= rows <= 2^31 - 2^16                     */
     int64_t x_stride, w_stride;    /* >= k, and at most 2^40, rows (n) * stride at most 2^44 */
     int64_t res_stride, y_stride;  /* >= n, likewise                               */
-    int32_t k, n;                  /* 1 <= k <= 131071 (the int32 sum is safe for any bytes), 1 <= n */
+    int32_t k, n;                  /* 1 <= k <= 131071 (the int32 sum is safe for any bytes), 1 <= n <= 2^31 - 2^16 */
     int32_t act;                   /* icnn_act                                     */
     int32_t dtype;                 /* of y and residual: ICNN_F32, F16 or BF16     */
 } icnn_linear_desc;

@@ -10,7 +10,7 @@ namespace {
 
 static_assert(kF32 == ICNN_F32 && kF16 == ICNN_F16 && kBf16 == ICNN_BF16, "types of a stream");
 
-constexpr int64_t kMostRows = 0x7fffffff, kMostStride = (int64_t)1 << 40, kMostElements = (int64_t)1 << 44;      // (16 TiB of bytes)
+constexpr int64_t kMostRows = 0x7fff0000, kMostStride = (int64_t)1 << 40, kMostElements = (int64_t)1 << 44;      // (16 TiB of bytes)
 
 int item_of(int dtype) { return dtype == ICNN_F32 ? 4 : 2; }
 
@@ -62,7 +62,7 @@ int launched(hipError_t e, const char *what)
 int check_rows_desc(const icnn_norm_desc *d)
 {
     if (!d) return fail(ICNN_E_NULL, "descriptor is NULL");
-    if (d->rows < 0 || d->rows > kMostRows) return fail(ICNN_E_SHAPE, "rows %lld must be in [0, 2^31)", (long long)d->rows);
+    if (d->rows < 0 || d->rows > kMostRows) return fail(ICNN_E_SHAPE, "rows %lld must be in [0, 2^31 - 2^16]", (long long)d->rows);
     if (d->c < 1 || d->c > (1 << 20)) return fail(ICNN_E_SHAPE, "c %d must be in [1, 2^20]", d->c);
     if (!is_stream(d->dtype)) return fail(ICNN_E_PARAM, "dtype %d must be ICNN_F32, ICNN_F16 or ICNN_BF16", d->dtype);
     int rc = check_stride("x_stride", d->x_stride, d->c, d->rows);
@@ -72,8 +72,8 @@ int check_rows_desc(const icnn_norm_desc *d)
 int check_linear(const icnn_linear_desc *d)
 {
     if (!d) return fail(ICNN_E_NULL, "descriptor is NULL");
-    if (d->rows < 0 || d->rows > kMostRows) return fail(ICNN_E_SHAPE, "rows %lld must be in [0, 2^31)", (long long)d->rows);
-    if (d->k < 1 || d->n < 1) return fail(ICNN_E_SHAPE, "k and n must be >= 1");
+    if (d->rows < 0 || d->rows > kMostRows) return fail(ICNN_E_SHAPE, "rows %lld must be in [0, 2^31 - 2^16]", (long long)d->rows);
+    if (d->k < 1 || d->n < 1 || d->n > kMostRows) return fail(ICNN_E_SHAPE, "k and n must be >= 1, n at most 2^31 - 2^16");
     if (d->k > 131071) return fail(ICNN_E_SHAPE, "k = %d exceeds 131071: int32 accumulation not provably safe", d->k);
     if (!is_stream(d->dtype)) return fail(ICNN_E_PARAM, "dtype %d must be ICNN_F32, ICNN_F16 or ICNN_BF16", d->dtype);
     if (d->act < ICNN_ACT_NONE || d->act > ICNN_ACT_GELU_TANH) return fail(ICNN_E_PARAM, "unknown act %d", d->act);

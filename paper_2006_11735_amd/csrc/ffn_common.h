@@ -29,6 +29,9 @@ struct LinearArgs {
     int act, dtype;
 };
 
+// A launch holds fewer than 2^32 threads
+constexpr bool fits_launch(long long groups, int threads) { return groups <= 0xffffffffLL / threads; }
+
 hipError_t launch_rows(const RowsArgs &a, hipStream_t st);
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st);
 size_t linear_workspace(const LinearArgs &a);

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(const LinearArgs a)
         if (DIRECT) {
             copy(t + DEPTH - 1);                           // into the stage that the last turn has read (its fragments have left it)
             asm volatile("" ::: "memory");
-            FFN_WAIT_VMCNT(COPIES + XL);                   // this turn's rows, and its weights, which were asked for before them or with them
+            FFN_WAIT_VMCNT(XL + COPIES);                   // all but the next turn's rows and weights (tests/test_few_waits.py counts them in the built kernels)
             asm volatile("" ::: "memory");
         } else {
             put(t);
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(const LinearArgs a)
 }
 
 // A tile's rows within 2 GiB of its first; k is at least a piece
-bool few_linear_takes(const LinearArgs &a) { return a.M <= 64 && a.K >= 16 && a.ldw <= (1 << 26); }
+bool few_linear_takes(const LinearArgs &a) { return a.M <= 64 && a.K >= 16 && a.ldw <= (1 << 26) && fits_launch((a.N + 15) / 16, NW * 64); }
 
 // Measured: a start and end and so much a megabyte of weights, or a turn of a wave where few workgroups are on the chip, by how many groups of 16 rows read each
 // (16 rows, 4096 -> 4096: 6.3 us; gated 4096 -> 16384: 32 us; 24 rows, 2048 -> 8192: 9.1 us, 16384 -> 2048: 16.7 us; 64 rows, 4096 -> 4096: 13.5 us, 16384 -> 512: 35 us)

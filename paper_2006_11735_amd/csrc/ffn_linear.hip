@@ -67,7 +67,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t st)
     }
     const int tiles_n = (a.N + 15) / 16;
     const long long tiles = (long long)((a.M + 15) / 16) * tiles_n, blocks = (tiles + 3) / 4;
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (!fits_launch(blocks, 256)) return hipErrorInvalidConfiguration;
     if (a.w2) hipLaunchKernelGGL(linear_plain_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, a, tiles_n, tiles);
     else hipLaunchKernelGGL(linear_plain_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, a, tiles_n, tiles);
     return hipGetLastError();

@@ -221,13 +221,32 @@ static hipError_t launch_rows_of(const RowsArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_rows(const RowsArgs &a, hipStream_t st)
+static hipError_t launch_some_rows(const RowsArgs &a, hipStream_t st)
 {
     const bool f32_gamma = a.gamma_dtype == kF32;
     if (!a.gamma) return a.dtype == kF32 ? launch_rows_of<kF32, 0>(a, st) : a.dtype == kF16 ? launch_rows_of<kF16, 0>(a, st) : launch_rows_of<kBf16, 0>(a, st);
     if (a.dtype == kF32) return launch_rows_of<kF32, kF32>(a, st);
     if (a.dtype == kF16) return f32_gamma ? launch_rows_of<kF16, kF32>(a, st) : launch_rows_of<kF16, kF16>(a, st);
     return f32_gamma ? launch_rows_of<kBf16, kF32>(a, st) : launch_rows_of<kBf16, kBf16>(a, st);
+}
+
+// (rows that one launch does not hold go in several)
+hipError_t launch_rows(const RowsArgs &a, hipStream_t st)
+{
+    constexpr long long MOST = 1 << 21;
+    static_assert(fits_launch(MOST, 1024), "a workgroup a row");
+    const int item = a.dtype == kF32 ? 4 : 2;
+    for (long long at = 0; at < a.rows; at += MOST) {
+        RowsArgs b = a;
+        b.rows = a.rows - at < MOST ? a.rows - at : MOST;
+        b.x = (const uint8_t *)a.x + at * a.ldx * item;
+        if (a.res) b.res = (const uint8_t *)a.res + at * a.ldr * item;
+        if (a.sum) b.sum = (uint8_t *)a.sum + at * a.lds * item;
+        b.q = a.q + at * a.ldq;
+        b.scale = a.scale + at;
+        if (hipError_t e = launch_some_rows(b, st)) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace icnn

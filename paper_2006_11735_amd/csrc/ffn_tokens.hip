@@ -108,7 +108,7 @@ __global__ __launch_bounds__(256) void linear_tokens_kernel(const LinearArgs a)
     }
 }
 
-bool tokens_linear_takes(const LinearArgs &a) { return a.M <= 4 && a.K >= 16 && a.K <= 32768; }
+bool tokens_linear_takes(const LinearArgs &a) { return a.M <= 4 && a.K >= 16 && a.K <= 32768 && fits_launch(a.N, 256); }
 
 template <int MR, int C, int KW, int OUT>
 static void launch_tokens(const LinearArgs &a, hipStream_t st)

@@ -74,7 +74,7 @@ W, WS, BI, Y, W2, WS2 = (k << 24 for k in range(11, 17))
 
 
 @pytest.mark.parametrize("kw,want", [
-    (dict(rows=-1), B.ICNN_E_SHAPE), (dict(rows=1 << 31), B.ICNN_E_SHAPE), (dict(k=0), B.ICNN_E_SHAPE), (dict(n=0), B.ICNN_E_SHAPE), (dict(k=131072), B.ICNN_E_SHAPE),
+    (dict(rows=-1), B.ICNN_E_SHAPE), (dict(rows=1 << 31), B.ICNN_E_SHAPE), (dict(k=0), B.ICNN_E_SHAPE), (dict(n=0), B.ICNN_E_SHAPE), (dict(n=(1 << 31) - 1, y_stride=1 << 31), B.ICNN_E_SHAPE), (dict(k=131072), B.ICNN_E_SHAPE),
     (dict(x_stride=63), B.ICNN_E_SHAPE), (dict(w_stride=63), B.ICNN_E_SHAPE), (dict(y_stride=31), B.ICNN_E_SHAPE), (dict(res_stride=31), B.ICNN_E_SHAPE),
     (dict(w_stride=1 << 41), B.ICNN_E_SHAPE), (dict(rows=1 << 30, y_stride=1 << 20), B.ICNN_E_SHAPE),
     (dict(dtype=B.ICNN_S8), B.ICNN_E_PARAM), (dict(dtype=-1), B.ICNN_E_PARAM), (dict(act=5), B.ICNN_E_PARAM), (dict(act=-1), B.ICNN_E_PARAM)])

@@ -168,3 +168,15 @@ def test_on_a_stream_of_its_own():
     st = torch.cuda.Stream()
     q, scale, s, gamma = run_norm(40, 2048, "f16", stream=st)
     check(q, scale, s, gamma, 1e-5)
+
+
+def test_more_rows_than_one_launch_takes():
+    rows, c = (1 << 21) + 5, 8
+    x = torch.randn((rows, c), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.float16)
+    q, scale, total = torch.empty((rows, c), dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x)
+    B.irms_norm_s8(B.norm_desc(rows=rows, c=c, dtype=B.ICNN_F16), x, x, torch.ones(c, dtype=torch.float16, device="cuda"), total, q, scale)
+    torch.cuda.synchronize()
+    for part in (slice(0, 300), slice((1 << 21) - 100, rows)):
+        s = (x[part].float() * 2).to(torch.float16)
+        assert torch.equal(total[part], s)
+        check(to_numpy(q[part]).astype(np.int64), to_numpy(scale[part]), to_numpy(s), np.ones(c), 1e-5)
