@@ -471,7 +471,7 @@ constexpr TileCost kTiles[] = {
     {128, 128, 512, 6.f, 0.58f, 1.25f},     // two workgroups on a compute unit
     {128, 128, 256, 8.5f, 0.48f, 0.58f},    // ... one, with four stages instead of two: 1024 x 4096 -> 4096: 26 us (the one before 35, the next one 30)
     {64, 128, 512, 4.f, 0.29f, 0.75f},      // gated 77 x 2048 -> 5461: 9.4 us (the next one 10.2)
-    {64, 64, 512, 3.f, 0.22f, 0.46f},       // 128 x 4096 -> 4096: 10.2 us (the one before 13.9), 512 x 4096 -> 4096: 16.4 us (16.3)
+    {64, 64, 512, 3.f, 0.22f, 0.46f},       // 128 x 4096 -> 4096: 10.2 us (the one before 13.9), 512 x 4096 -> 4096: 16.4 us (16.3); gated, by half the waves, 1.5 us more
 };
 constexpr int kTileKinds = sizeof(kTiles) / sizeof(kTiles[0]);
 constexpr int kMostSplits = 16, kSplitTiles = (int)(kWsCounterBytes / sizeof(unsigned));
@@ -494,8 +494,10 @@ static TilePlan plan_tiles(const LinearArgs &a, bool may_split)
         const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + t.n - 1) / t.n);
         for (int s = 1; s <= kMostSplits; ++s) {
             if (s > 1 && (!may_split || tiles > (float)kSplitTiles || tiles * (float)s > (float)t.held || 2 * s > steps)) break;
-            const float units = tiles * (float)s, turns = __builtin_ceilf(units / (float)t.held), full = units < (float)t.held ? units / (float)t.held : 1.f;
-            const float us = turns * (t.fixed + (float)((steps + s - 1) / s) * (t.few + (t.all - t.few) * full)) + (s > 1 ? kExchange + kExchangeRange * (float)s + kExchangeSums * units * (float)(t.m * t.n / 4096) : 0.f);
+            // (one workgroup on each unit: all of the chip, or, of the tiles that two share a unit, a quarter of the way there)
+            const float units = tiles * (float)s, turns = __builtin_ceilf(units / (float)t.held), on = units < (float)t.held ? units / 256.f : (float)t.held / 256.f;
+            const float full = t.held == 256 ? on : on < 1.f ? 0.25f * on : 0.25f + 0.75f * (on - 1.f), more = c == kTileKinds - 1 && a.w2 ? 1.5f : 0.f;
+            const float us = turns * (t.fixed + more + (float)((steps + s - 1) / s) * (t.few + (t.all - t.few) * full)) + (s > 1 ? kExchange + kExchangeRange * (float)s + kExchangeSums * units * (float)(t.m * t.n / 4096) : 0.f);
             if (g_tuning.ff_split ? s == 1 || s <= g_tuning.ff_split : best.us == 0.f || us < best.us) best = {c, s, us};
         }
     }

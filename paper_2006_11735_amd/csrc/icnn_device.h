@@ -9,9 +9,6 @@ namespace icnn {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v16i __attribute__((ext_vector_type(16)));
 
-// Notes the message of the calling thread's last failure, returns `code` (see api.hip)
-int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
-
 // Packed weight format: the cout axis is cut into chunks of 32 output channels and
 // the K = kh*kw*cin axis (order kh, kw, ci) into steps of 64.  One (chunk, step) pair
 // is 2048 bytes: [k32 half][lane 0..63][16 bytes], exactly the A-operand fragments
