@@ -41,6 +41,16 @@ __device__ __forceinline__ int piece_key(int q)
 // are read and moved down.
 __device__ __forceinline__ v4i last_k16(const int8_t *p, int left) { return move_down(*(const v4i_any *)(p - max(16 - left, 0)), left); }
 
+// fn(0) ... fn(N - 1), the numbers as constants
+template <int N, class F>
+__device__ __forceinline__ void times(std::integral_constant<int, N>, F &&fn)
+{
+    if constexpr (N > 0) {
+        times(std::integral_constant<int, N - 1>{}, fn);
+        fn(std::integral_constant<int, N - 1>{});
+    }
+}
+
 // Waves a SIMD when as many workgroups of `waves` waves as their LDS lets share a compute unit do (three at most: the registers are wanted too)
 constexpr int waves_per_simd(int waves, int lds_bytes)
 {
@@ -122,9 +132,12 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
             }
         }
     };
-    // The same through registers, for rows that start anywhere: fetch_step's loads are in flight while a stage is multiplied, put_step's stores follow
-    v4i held[LOADS];
-    auto fetch_step = [&](int s) {
+    // The same through registers, for rows that start anywhere: the loads of AHEAD steps (as many as there are registers for) are in flight while a stage is multiplied,
+    // put_step's stores follow
+    constexpr int AHEAD = DIRECT || TN * TM > 4 ? 1 : LOADS <= 4 ? 4 : 2;
+    v4i held_of[AHEAD][LOADS];
+    auto fetch_step = [&](int s, auto slot) {
+        v4i(&held)[LOADS] = held_of[slot];
         const int k0 = first + s * BK;
         const int8_t *const w0 = a.w + n0 * a.ldw + k0, *const w1 = (GATED ? a.w2 : a.w) + n0 * a.ldw + k0, *const x0 = a.x + m0 * a.ldx + k0;
         if (k0 + BK <= a.K) {
@@ -146,7 +159,8 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
             for (int j = 0; j < LX; ++j) held[LW + j] = last_k16(x0 + off_x[j], left - 16 * piece_x[j]);
         }
     };
-    auto put_step = [&](int s) {
+    auto put_step = [&](int s, auto slot) {
+        const v4i(&held)[LOADS] = held_of[slot];
         uint8_t *const to = lds + (s % STAGES) * STAGE + wave * 1024 + lane * 16;
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) *(v4i *)(to + (j < LW ? j * NW * 1024 : BN * BK + (j - LW) * NW * 1024)) = held[j];
@@ -199,9 +213,11 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
             else copy_part(s, None{}, Half{});
         FFN_WAIT_VMCNT((STAGES - 2) * LOADS + LOADS / 2);
     } else {
-        fetch_step(0);
-        put_step(0);
-        if (1 < steps) fetch_step(1);
+        times(std::integral_constant<int, AHEAD>{}, [&](auto u) {
+            if (u < steps) fetch_step(u, u);
+        });
+        put_step(0, None{});
+        if (AHEAD < steps) fetch_step(AHEAD, None{});
         FFN_WAIT_LGKM();
     }
     asm volatile("" ::: "memory");
@@ -210,7 +226,7 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
     read_slice(0, 0, 0);
     // A stage's last slice is multiplied behind the barrier: its fragments have left LDS in front of it, so the stage is free for the copies of the step STAGES
     // further on (half of them there, half in the next step's first slice), and the first fragments of the next step come in under those products.
-    for (int s = 0; s < steps; ++s) {
+    auto one_step = [&](int s, auto next) {                // next: the slot of step s + 1
 #pragma unroll
         for (int kk = 0; kk < SLICES - 1; ++kk) {
             read_slice(s % STAGES, kk + 1, (kk + 1) & 1);
@@ -220,17 +236,21 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
             else order(None{});
         }
         if (DIRECT) FFN_WAIT_VMCNT((STAGES - 2) * LOADS);              // (the stages behind the next one are still in flight)
-        else if (s + 1 < steps) put_step(s + 1);
+        else if (s + 1 < steps) put_step(s + 1, next);
         FFN_WAIT_LGKM();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         read_slice((s + 1) % STAGES, 0, 0);
         if (DIRECT) copy_part(s + STAGES, None{}, Half{});
-        else if (s + 2 < steps) fetch_step(s + 2);
+        else if (s + 1 + AHEAD < steps) fetch_step(s + 1 + AHEAD, next);
         multiply(1);
         if (DIRECT) order(Half{});
-    }
+    };
+    for (int s = 0; s < steps; s += AHEAD)
+        times(std::integral_constant<int, AHEAD>{}, [&](auto u) {
+            if (u == 0 || s + u < steps) one_step(s + u, std::integral_constant<int, (u + 1) % AHEAD>{});
+        });
     FFN_WAIT_VMCNT(0);
     drain(acc);
 
