@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void linear_plain_kernel(const LinearArgs a, i
     finish_four<GATED>(a, acc[0], acc[1], f, m, n0 + 4 * g);
 }
 
-// Up to four rows go token by token (1 x 16384 -> 4096: 12.5 us, by the kernel for few rows 17; 4 rows: 16.3 and 17.2), the others where they take least by what
+// Up to four rows go token by token (1 x 16384 -> 4096: 12.3 us, by the kernel for few rows 16.1; 4 rows: 14.0 and 16.4), the others where they take least by what
 // has been measured; what none of those takes (k below 16, rows gigabytes apart) by the plain kernel.
 enum Kernel { kPlain, kTokens, kFew, kTiled };
 static Kernel choose(const LinearArgs &a, bool may_split)
