@@ -177,12 +177,14 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(const LinearArgs a)
 // A tile's rows within 2 GiB of its first; k is at least a piece
 bool few_linear_takes(const LinearArgs &a) { return a.M <= 64 && a.K >= 16 && a.ldw <= (1 << 26) && fits_launch((a.N + 15) / 16, NW * 64); }
 
-// Measured: a start and end and so much a megabyte of weights, or a turn of a wave where few workgroups are on the chip, by how many groups of 16 rows read each
-// (16 rows, 4096 -> 4096: 6.3 us; gated 4096 -> 16384: 32 us; 24 rows, 2048 -> 8192: 9.1 us, 16384 -> 2048: 16.7 us; 64 rows, 4096 -> 4096: 13.5 us, 16384 -> 512: 35 us)
+// Measured: a start, so much a megabyte of weights and so much for each time that the chip is filled with workgroups (each reads all rows; gated ones do it for
+// twice the weights), or a turn of a wave where few workgroups are on the chip (8 rows, 4096 -> 16384: 16.1 us, 8192 -> 8192: 14.7, gated 4096 -> 16384: 26.1; 16 rows,
+// 4096 -> 4096: 7.4, 1024 -> 16384: 9.0; 32 rows, 16384 -> 4096: 23, 4096 -> 16384: 27.7; 64 rows, 4096 -> 4096: 13.5, 16384 -> 512: 35)
 float few_linear_us(const LinearArgs &a)
 {
     const float mb = (a.w2 ? 2.f : 1.f) * (float)a.N * (float)a.K * 1e-6f, turns = (float)((a.K + NW * RB - 1) / (NW * RB));
-    const float flow = a.M <= 16 ? 3.2f + 0.2f * mb : a.M <= 32 ? 5.f + 0.215f * mb : 6.5f + 0.47f * mb;
+    const float fills = (a.w2 ? 0.5f : 1.f) * (float)a.N / 4096.f;
+    const float flow = a.M <= 8 ? 3.f + 0.165f * mb + 0.35f * fills : a.M <= 16 ? 3.f + 0.19f * mb + 0.9f * fills : a.M <= 32 ? 3.f + 0.21f * mb + 2.2f * fills : 6.5f + 0.47f * mb;
     const float chain = 3.f + turns * (a.M <= 16 ? 0.8f : a.M <= 32 ? 0.85f : 2.f);
     return flow > chain ? flow : chain;
 }
