@@ -39,6 +39,13 @@ size_t linear_workspace(const LinearArgs &a);
 bool tokens_linear_takes(const LinearArgs &a);
 hipError_t launch_tokens_linear(const LinearArgs &a, hipStream_t st);
 bool few_linear_takes(const LinearArgs &a);
+// How much longer a step along k is where rows go through registers: 64 x 5456 -> 2048 (rows at multiples of 16) 15.2 us, 5464 (of 8) 15.9, 5461 19.7; 4096 x 2048 ->
+// 8192 in 256 x 256 tiles 86 us, 2047 115
+inline float step_factor(const LinearArgs &a)
+{
+    const unsigned at = (unsigned)((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.w2) | (unsigned)(a.ldx | a.ldw);
+    return at & 3 ? 1.7f : (at | (unsigned)a.K) & 15 ? 1.2f : 1.f;
+}
 float few_linear_us(const LinearArgs &a);
 hipError_t launch_few_linear(const LinearArgs &a, hipStream_t st);
 bool tiled_linear_takes(const LinearArgs &a);
@@ -201,20 +208,15 @@ __device__ __forceinline__ void load_column(const float *p, int n, int N, float 
     for (int e = 0; e < 8; ++e) v[e] = value_of<kF32>(t, e);
 }
 
-// The last 16 numbers of a row, moved down so that they stand for the 16 of which `left` are left in the row, zeros behind them (left >= 16: as they are)
-__device__ __forceinline__ v4i move_down(const v4i &v, int left)
+// A piece of k that goes beyond a row's end is read as the row's last 16 numbers, in both operands alike, so that each still meets its own.  What is left of the row
+// (16: all of them, 0 or less: none) is its last `left` numbers, the others have been in the piece before: in the rows, not the weights, they are made zeros.
+__device__ __forceinline__ v4i last_of(const v4i &v, int left)
 {
-    const int over = min(max(16 - left, 0), 16);
     v4i r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        int lo = 0, hi = 0;
-#pragma unroll
-        for (int q = i; q < 4; ++q) {
-            lo = q == i + (over >> 2) ? v[q] : lo;
-            hi = q == i + (over >> 2) + 1 ? v[q] : hi;
-        }
-        r[i] = (int)__builtin_amdgcn_alignbyte((uint32_t)hi, (uint32_t)lo, (uint32_t)(over & 3));
+        const int over = 16 - left - 4 * i;                // numbers of these four to clear
+        r[i] = over >= 4 ? 0 : (int)((unsigned)v[i] & 0xffffffffu << (8 * max(over, 0)));
     }
     return r;
 }

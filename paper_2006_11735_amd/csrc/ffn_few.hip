@@ -64,24 +64,15 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(const LinearArgs a)
             for (int i = 0; i < CP; ++i)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[l], (LdsVoid *)(to + l * WB + i * 1024), 16, 16 * piece[i] < left ? off[i] : 0x80000000u, k0, 0, 2);      // (2: not to be kept)
     };
-    // the same through registers, for rows that start anywhere
+    // the same through registers, for rows that start anywhere (no load hangs on a condition, behind which the compiler would wait for all loads in flight)
     v4i held[COPIES];
     auto fetch = [&](int t) {
         const int k0 = (wave + t * NW) * RB;
 #pragma unroll
-        for (int l = 0; l < L; ++l) {
-            const int8_t *const w = (l ? a.w2 : a.w) + n0 * a.ldw + k0;
-            if (k0 + RB <= a.K) {
+        for (int l = 0; l < L; ++l)
 #pragma unroll
-                for (int i = 0; i < CP; ++i) held[CP * l + i] = *(const v4i_any *)(w + off[i]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < CP; ++i) {
-                    const int left = a.K - k0 - 16 * piece[i];
-                    held[CP * l + i] = move_down(*(const v4i_any *)(w + off[i] - max(16 - left, 0)), left);
-                }
-            }
-        }
+            for (int i = 0; i < CP; ++i)
+                held[CP * l + i] = *(const v4i_any *)((l ? a.w2 : a.w) + n0 * a.ldw + (off[i] + (unsigned)min(k0, a.K - 16 - 16 * piece[i])));
     };
     auto put = [&](int t) {
 #pragma unroll
@@ -128,13 +119,13 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(const LinearArgs a)
             asm volatile("" ::: "memory");
         } else {
             put(t);
-            if (t + 1 < mine) fetch(t + 1);
+            fetch(t + 1);
             const int k0 = (wave + t * NW) * RB;
-            if (k0 + RB > a.K) {                          // (whole pieces meet weights that are zero; a part of one is where its weights are)
+            if (k0 + RB > a.K) {
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int q = 0; q < XQ; ++q) xv[set][i][q] = move_down(xv[set][i][q], a.K - k0 - 64 * q - 16 * g);
+                    for (int q = 0; q < XQ; ++q) xv[set][i][q] = last_of(xv[set][i][q], a.K - k0 - 64 * q - 16 * g);
             }
         }
         const uint8_t *const from = ring + (t % DEPTH) * STAGE + r * RB;
@@ -186,7 +177,10 @@ float few_linear_us(const LinearArgs &a)
     const float fills = (a.w2 ? 0.5f : 1.f) * (float)a.N / 4096.f;
     const float flow = a.M <= 8 ? 3.f + 0.165f * mb + 0.35f * fills : a.M <= 16 ? 3.f + 0.19f * mb + 0.9f * fills : a.M <= 32 ? 3.f + 0.21f * mb + 2.2f * fills : 6.5f + 0.47f * mb;
     const float chain = 3.f + turns * (a.M <= 16 ? 0.8f : a.M <= 32 ? 0.85f : 2.f);
-    return flow > chain ? flow : chain;
+    // (loads at odd places hold up a compute unit's other ones: 8 and 16 rows, 5461 -> 5000: 17.9 and 23.3 us, 5461 -> 2048: 10 and 12.6)
+    const float step = step_factor(a), slow = step < 1.5f ? step : a.M <= 8 ? 2.f : a.M <= 16 ? 2.6f : 3.2f, slow_chain = step < 1.5f ? step : 0.7f * slow;
+    const float by_flow = slow * (flow - 3.f), by_chain = slow_chain * (chain - 3.f);
+    return 3.f + (by_flow > by_chain ? by_flow : by_chain);
 }
 
 template <int MT, bool GATED, bool DIRECT>

@@ -37,10 +37,6 @@ __device__ __forceinline__ int piece_key(int q)
     return WEIGHTS ? ((q >> 2) & 1) | ((q >> 4) & 1) << 1 : (q >> 2) & 3;
 }
 
-// The 16 numbers from p on of a row of which `left` are left (any number, also none or less), zeros behind them.  The row has 16 numbers at least: its last 16
-// are read and moved down.
-__device__ __forceinline__ v4i last_k16(const int8_t *p, int left) { return move_down(*(const v4i_any *)(p - max(16 - left, 0)), left); }
-
 // fn(0) ... fn(N - 1), the numbers as constants
 template <int N, class F>
 __device__ __forceinline__ void times(std::integral_constant<int, N>, F &&fn)
@@ -133,35 +129,31 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
         }
     };
     // The same through registers, for rows that start anywhere: the loads of AHEAD steps (as many as there are registers for) are in flight while a stage is multiplied,
-    // put_step's stores follow
+    // put_step's stores follow.  No load hangs on a condition: the compiler then counts the loads in flight, behind a branch it would wait for all of them.  A piece
+    // that goes beyond the row's end is its last 16 numbers, in both operands; put_step clears those of the rows' that have been before, or all behind the end.
     constexpr int AHEAD = DIRECT || TN * TM > 4 ? 1 : LOADS <= 4 ? 4 : 2;
     v4i held_of[AHEAD][LOADS];
     auto fetch_step = [&](int s, auto slot) {
         v4i(&held)[LOADS] = held_of[slot];
         const int k0 = first + s * BK;
-        const int8_t *const w0 = a.w + n0 * a.ldw + k0, *const w1 = (GATED ? a.w2 : a.w) + n0 * a.ldw + k0, *const x0 = a.x + m0 * a.ldx + k0;
-        if (k0 + BK <= a.K) {
+        const unsigned some = s < steps ? ~0u : 0u;        // (behind the last step all lanes read one place, which costs less)
+        const int8_t *const w0 = a.w + n0 * a.ldw, *const w1 = (GATED ? a.w2 : a.w) + n0 * a.ldw, *const x0 = a.x + m0 * a.ldx;
 #pragma unroll
-            for (int j = 0; j < LW; ++j) {
-                const bool up = GATED && (((j * NW + wave) * ROWS) & 32);
-                held[j] = *(const v4i_any *)((up ? w1 : w0) + off_w[j]);
-            }
-#pragma unroll
-            for (int j = 0; j < LX; ++j) held[LW + j] = *(const v4i_any *)(x0 + off_x[j]);
-        } else {
-            const int left = a.K - k0;
-#pragma unroll
-            for (int j = 0; j < LW; ++j) {
-                const bool up = GATED && (((j * NW + wave) * ROWS) & 32);
-                held[j] = last_k16((up ? w1 : w0) + off_w[j], left - 16 * piece_w[j]);
-            }
-#pragma unroll
-            for (int j = 0; j < LX; ++j) held[LW + j] = last_k16(x0 + off_x[j], left - 16 * piece_x[j]);
+        for (int j = 0; j < LW; ++j) {
+            const bool up = GATED && (((j * NW + wave) * ROWS) & 32);
+            held[j] = *(const v4i_any *)((up ? w1 : w0) + ((off_w[j] + (unsigned)min(k0, a.K - 16 - 16 * piece_w[j])) & some));
         }
+#pragma unroll
+        for (int j = 0; j < LX; ++j) held[LW + j] = *(const v4i_any *)(x0 + ((off_x[j] + (unsigned)min(k0, a.K - 16 - 16 * piece_x[j])) & some));
     };
     auto put_step = [&](int s, auto slot) {
-        const v4i(&held)[LOADS] = held_of[slot];
+        v4i(&held)[LOADS] = held_of[slot];
         uint8_t *const to = lds + (s % STAGES) * STAGE + wave * 1024 + lane * 16;
+        const int left = a.K - first - s * BK;
+        if (left < BK) {
+#pragma unroll
+            for (int j = 0; j < LX; ++j) held[LW + j] = last_of(held[LW + j], left - 16 * piece_x[j]);
+        }
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) *(v4i *)(to + (j < LW ? j * NW * 1024 : BN * BK + (j - LW) * NW * 1024)) = held[j];
     };
@@ -213,11 +205,9 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
             else copy_part(s, None{}, Half{});
         FFN_WAIT_VMCNT((STAGES - 2) * LOADS + LOADS / 2);
     } else {
-        times(std::integral_constant<int, AHEAD>{}, [&](auto u) {
-            if (u < steps) fetch_step(u, u);
-        });
+        times(std::integral_constant<int, AHEAD>{}, [&](auto u) { fetch_step(u, u); });
         put_step(0, None{});
-        if (AHEAD < steps) fetch_step(AHEAD, None{});
+        fetch_step(AHEAD, None{});
         FFN_WAIT_LGKM();
     }
     asm volatile("" ::: "memory");
@@ -226,7 +216,7 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
     read_slice(0, 0, 0);
     // A stage's last slice is multiplied behind the barrier: its fragments have left LDS in front of it, so the stage is free for the copies of the step STAGES
     // further on (half of them there, half in the next step's first slice), and the first fragments of the next step come in under those products.
-    auto one_step = [&](int s, auto next) {                // next: the slot of step s + 1
+    auto one_step = [&](int s, auto next, auto more) {     // next: the slot of step s + 1; more: whether to load into it what comes AHEAD steps later
 #pragma unroll
         for (int kk = 0; kk < SLICES - 1; ++kk) {
             read_slice(s % STAGES, kk + 1, (kk + 1) & 1);
@@ -236,21 +226,23 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
             else order(None{});
         }
         if (DIRECT) FFN_WAIT_VMCNT((STAGES - 2) * LOADS);              // (the stages behind the next one are still in flight)
-        else if (s + 1 < steps) put_step(s + 1, next);
+        else put_step(s + 1, next);
         FFN_WAIT_LGKM();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         read_slice((s + 1) % STAGES, 0, 0);
         if (DIRECT) copy_part(s + STAGES, None{}, Half{});
-        else if (s + 1 + AHEAD < steps) fetch_step(s + 1 + AHEAD, next);
+        else if (more) fetch_step(s + 1 + AHEAD, next);
         multiply(1);
         if (DIRECT) order(Half{});
     };
-    for (int s = 0; s < steps; s += AHEAD)
-        times(std::integral_constant<int, AHEAD>{}, [&](auto u) {
-            if (u == 0 || s + u < steps) one_step(s + u, std::integral_constant<int, (u + 1) % AHEAD>{});
-        });
+    int s = 0;
+    for (; s + AHEAD <= steps; s += AHEAD)
+        times(std::integral_constant<int, AHEAD>{}, [&](auto u) { one_step(s + u, std::integral_constant<int, (u + 1) % AHEAD>{}, std::true_type{}); });
+    times(std::integral_constant<int, AHEAD - 1>{}, [&](auto u) {
+        if (s + u < steps) one_step(s + u, std::integral_constant<int, u + 1>{}, std::false_type{});
+    });
     FFN_WAIT_VMCNT(0);
     drain(acc);
 
@@ -508,16 +500,18 @@ static TilePlan plan_tiles(const LinearArgs &a, bool may_split)
 {
     TilePlan best = {0, 1, 0.f};
     const int steps = (a.K + 127) / 128;
+    const float step = step_factor(a);
     for (int c = 0; c < kTileKinds; ++c) {
         if (g_tuning.ff_kernel >= 4 && c != g_tuning.ff_kernel - 4) continue;
         const TileCost &t = kTiles[c];
         const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + t.n - 1) / t.n);
         for (int s = 1; s <= kMostSplits; ++s) {
             if (s > 1 && (!may_split || tiles > (float)kSplitTiles || tiles * (float)s > (float)t.held || 2 * s > steps)) break;
-            // (one workgroup on each unit: all of the chip, or, of the tiles that two share a unit, a quarter of the way there)
+            // (one workgroup on each unit: all of the chip, or, of the tiles that two share a unit, a quarter of the way there; through registers less of it, and
+            // all where any unit has two: 384 x 5461 -> 2048 in 64 x 64 tiles 0.36 us a step, 1000 x 5461 -> 2048 0.73)
             const float units = tiles * (float)s, turns = __builtin_ceilf(units / (float)t.held), on = units < (float)t.held ? units / 256.f : (float)t.held / 256.f;
-            const float full = t.held == 256 ? on : on < 1.f ? 0.25f * on : 0.25f + 0.75f * (on - 1.f), more = c == kTileKinds - 1 && a.w2 ? 1.5f : 0.f;
-            const float us = turns * (t.fixed + more + (float)((steps + s - 1) / s) * (t.few + (t.all - t.few) * full)) + (s > 1 ? kExchange + kExchangeRange * (float)s + kExchangeSums * units * (float)(t.m * t.n / 4096) : 0.f);
+            const float full = t.held == 256 ? on : step > 1.f ? (on > 1.f ? 1.f : 0.15f * on) : on < 1.f ? 0.25f * on : 0.25f + 0.75f * (on - 1.f), more = c == kTileKinds - 1 && a.w2 ? 1.5f : 0.f;
+            const float us = turns * (t.fixed + more + (float)((steps + s - 1) / s) * step * (t.few + (t.all - t.few) * full)) + (s > 1 ? kExchange + kExchangeRange * (float)s + kExchangeSums * units * (float)(t.m * t.n / 4096) : 0.f);
             if (g_tuning.ff_split ? s == 1 || s <= g_tuning.ff_split : best.us == 0.f || us < best.us) best = {c, s, us};
         }
     }

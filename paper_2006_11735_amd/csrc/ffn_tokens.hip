@@ -48,7 +48,7 @@ __global__ __launch_bounds__(64 * (KW > 4 ? KW : 4)) void linear_tokens_kernel(c
     __shared__ int part[NW][V];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n0 = ((int)blockIdx.x * (NW / KW) + wave / KW) * OUT;      // (may lie behind the last output: nothing is stored then)
-    // the pieces' places in a row; a piece that goes beyond its end is read as the row's last 16 bytes and moved down, zeros behind
+    // the pieces' places in a row, no further on than its last 16 bytes
     int at[C], left[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -56,7 +56,6 @@ __global__ __launch_bounds__(64 * (KW > 4 ? KW : 4)) void linear_tokens_kernel(c
         left[c] = a.K - k;
         at[c] = min(k, a.K - 16);
     }
-    const bool whole = (a.K & 15) == 0;
     v4i x[MR][C], w[OUT][L][C];
 #pragma unroll
     for (int m = 0; m < MR; ++m)
@@ -90,15 +89,7 @@ __global__ __launch_bounds__(64 * (KW > 4 ? KW : 4)) void linear_tokens_kernel(c
 #pragma unroll
     for (int m = 0; m < MR; ++m)
 #pragma unroll
-        for (int c = 0; c < C; ++c) x[m][c] = whole ? (left[c] > 0 ? x[m][c] : v4i{}) : move_down(x[m][c], left[c]);
-    if (!whole) {
-#pragma unroll
-        for (int b = 0; b < OUT; ++b)
-#pragma unroll
-            for (int l = 0; l < L; ++l)
-#pragma unroll
-                for (int c = 0; c < C; ++c) w[b][l][c] = move_down(w[b][l][c], left[c]);
-    }
+        for (int c = 0; c < C; ++c) x[m][c] = last_of(x[m][c], left[c]);
     int sum[V] = {};
 #pragma unroll
     for (int b = 0; b < OUT; ++b)
