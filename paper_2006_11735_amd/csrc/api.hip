@@ -1361,7 +1361,7 @@ int workspace_bytes(const icnn_linear_desc *desc, bool gated, size_t *bytes)
     LinearArgs a = {};
     sizes_of(desc, a);
     a.w2 = gated ? (const int8_t *)16 : nullptr;           // (whether there is one; never read)
-    *bytes = desc->rows ? linear_workspace(a) : 0;
+    *bytes = desc->rows ? linear_workspace(a, linear_tuning()) : 0;
     return ICNN_OK;
 }
 

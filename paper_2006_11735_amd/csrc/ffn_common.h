@@ -1,6 +1,7 @@
 // What the kernels of the feed-forward operators in 8 bits share: their arguments, numbers of the stream's types, activations.
 #pragma once
 #include "icnn_device.h"
+#include "ffn_plan.h"
 
 namespace icnn {
 
@@ -17,41 +18,14 @@ struct RowsArgs {
     float eps;
 };
 
-// A product of 8-bit rows and 8-bit weights, or the two of a gated layer (see ffn_linear.hip)
-struct LinearArgs {
-    const int8_t *x, *w, *w2;       // w2 null: one product.  Else y = act(first) * second
-    const float *xs, *ws, *ws2, *bias, *bias2;
-    const void *res;
-    void *y;
-    void *workspace;                // null: k stays whole
-    long long ldx, ldw, ldr, ldy;
-    int M, N, K;
-    int act, dtype;
-};
-
-// A launch holds fewer than 2^32 threads
-constexpr bool fits_launch(long long groups, int threads) { return groups <= 0xffffffffLL / threads; }
-
 hipError_t launch_rows(const RowsArgs &a, hipStream_t st);
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st);
-size_t linear_workspace(const LinearArgs &a);
-// kernels of ffn_tokens.hip, ffn_few.hip and ffn_tiled.hip: whether they take a product's shape, and about how long it takes them
-bool tokens_linear_takes(const LinearArgs &a);
+// kernels of ffn_tokens.hip, ffn_few.hip and ffn_tiled.hip
 hipError_t launch_tokens_linear(const LinearArgs &a, hipStream_t st);
-bool few_linear_takes(const LinearArgs &a);
-// How much longer a step along k is where rows go through registers: 64 x 5456 -> 2048 (rows at multiples of 16) 15.2 us, 5464 (of 8) 15.9, 5461 19.7; 4096 x 2048 ->
-// 8192 in 256 x 256 tiles 86 us, 2047 115
-inline float step_factor(const LinearArgs &a)
-{
-    const unsigned at = (unsigned)((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.w2) | (unsigned)(a.ldx | a.ldw);
-    return at & 3 ? 1.7f : (at | (unsigned)a.K) & 15 ? 1.2f : 1.f;
-}
-float few_linear_us(const LinearArgs &a);
 hipError_t launch_few_linear(const LinearArgs &a, hipStream_t st);
-bool tiled_linear_takes(const LinearArgs &a);
-float tiled_linear_us(const LinearArgs &a, bool may_split);
-size_t tiled_linear_workspace(const LinearArgs &a);      // of counters and partial sums
-hipError_t launch_tiled_linear(const LinearArgs &a, hipStream_t st);
+hipError_t launch_tiled_linear(const LinearArgs &a, const TilePlan &plan, hipStream_t st);
+
+inline LinearTuning linear_tuning() { return {g_tuning.ff_kernel, g_tuning.ff_split}; }
 
 typedef int v4i_any __attribute__((ext_vector_type(4), aligned(1)));       // (global memory takes 16 bytes at any address)
 typedef float v2f __attribute__((ext_vector_type(2)));

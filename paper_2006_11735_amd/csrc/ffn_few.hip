@@ -28,7 +28,7 @@ __device__ __forceinline__ void drain(v4i (&acc)[N])
 
 // Four waves of two stages: with eight, or more stages, fewer workgroups share a compute unit and less of one's start and end is under the others' copies
 // (16 rows, 4096 -> 4096: 6.3 us, with eight waves 7.4 to 8.2; turns of 512 bytes 8.2)
-constexpr int NW = 4, DEPTH = 2, RB = 256;
+constexpr int NW = kFewWaves, DEPTH = 2, RB = kFewTurn;
 
 }  // namespace
 
@@ -163,24 +163,6 @@ __global__ __launch_bounds__(NW * 64) void linear_few_kernel(const LinearArgs a)
         if (m < a.M) finish_four<GATED>(a, c, c2, f, m, n0 + 4 * g);
     }
 #endif
-}
-
-// A tile's rows within 2 GiB of its first; k is at least a piece
-bool few_linear_takes(const LinearArgs &a) { return a.M <= 64 && a.K >= 16 && a.ldw <= (1 << 26) && fits_launch((a.N + 15) / 16, NW * 64); }
-
-// Measured: a start, so much a megabyte of weights and so much for each time that the chip is filled with workgroups (each reads all rows; gated ones do it for
-// twice the weights), or a turn of a wave where few workgroups are on the chip (8 rows, 4096 -> 16384: 16.1 us, 8192 -> 8192: 14.7, gated 4096 -> 16384: 26.1; 16 rows,
-// 4096 -> 4096: 7.4, 1024 -> 16384: 9.0; 32 rows, 16384 -> 4096: 23, 4096 -> 16384: 27.7; 64 rows, 4096 -> 4096: 13.5, 16384 -> 512: 35)
-float few_linear_us(const LinearArgs &a)
-{
-    const float mb = (a.w2 ? 2.f : 1.f) * (float)a.N * (float)a.K * 1e-6f, turns = (float)((a.K + NW * RB - 1) / (NW * RB));
-    const float fills = (a.w2 ? 0.5f : 1.f) * (float)a.N / 4096.f;
-    const float flow = a.M <= 8 ? 3.f + 0.165f * mb + 0.35f * fills : a.M <= 16 ? 3.f + 0.19f * mb + 0.9f * fills : a.M <= 32 ? 3.f + 0.21f * mb + 2.2f * fills : 6.5f + 0.47f * mb;
-    const float chain = 3.f + turns * (a.M <= 16 ? 0.8f : a.M <= 32 ? 0.85f : 2.f);
-    // (loads at odd places hold up a compute unit's other ones: 8 and 16 rows, 5461 -> 5000: 17.9 and 23.3 us, 5461 -> 2048: 10 and 12.6)
-    const float step = step_factor(a), slow = step < 1.5f ? step : a.M <= 8 ? 2.f : a.M <= 16 ? 2.6f : 3.2f, slow_chain = step < 1.5f ? step : 0.7f * slow;
-    const float by_flow = slow * (flow - 3.f), by_chain = slow_chain * (chain - 3.f);
-    return 3.f + (by_flow > by_chain ? by_flow : by_chain);
 }
 
 template <int MT, bool GATED, bool DIRECT>

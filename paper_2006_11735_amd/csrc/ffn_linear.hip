@@ -43,27 +43,14 @@ __global__ __launch_bounds__(256) void linear_plain_kernel(const LinearArgs a, i
     finish_four<GATED>(a, acc[0], acc[1], f, m, n0 + 4 * g);
 }
 
-// Up to four rows go token by token (1 x 16384 -> 4096: 12.3 us, by the kernel for few rows 16.1; 4 rows: 14.0 and 16.4), the others where they take least by what
-// has been measured; what none of those takes (k below 16, rows gigabytes apart) by the plain kernel.
-enum Kernel { kPlain, kTokens, kFew, kTiled };
-static Kernel choose(const LinearArgs &a, bool may_split)
-{
-    const int force = g_tuning.ff_kernel;
-    const bool few = few_linear_takes(a), tiled = tiled_linear_takes(a);
-    if (tokens_linear_takes(a) && (force == 0 || force == 2)) return kTokens;
-    if (few && (force == 3 || (force == 0 && (!tiled || few_linear_us(a) < tiled_linear_us(a, may_split))))) return kFew;
-    return tiled && (force == 0 || force >= 4) ? kTiled : kPlain;
-}
-
-size_t linear_workspace(const LinearArgs &a) { return choose(a, true) == kTiled ? tiled_linear_workspace(a) : 0; }
-
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st)
 {
-    switch (choose(a, a.workspace != nullptr)) {
-    case kTokens: return launch_tokens_linear(a, st);
-    case kFew: return launch_few_linear(a, st);
-    case kTiled: return launch_tiled_linear(a, st);
-    case kPlain: break;
+    const LinearPlan plan = plan_launch(a, linear_tuning());
+    switch (plan.kernel) {
+    case LinearKernel::tokens: return launch_tokens_linear(a, st);
+    case LinearKernel::few: return launch_few_linear(a, st);
+    case LinearKernel::tiled: return launch_tiled_linear(a, plan.tiles, st);
+    case LinearKernel::plain: break;
     }
     const int tiles_n = (a.N + 15) / 16;
     const long long tiles = (long long)((a.M + 15) / 16) * tiles_n, blocks = (tiles + 3) / 4;

@@ -429,9 +429,6 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
 #endif
 }
 
-// Offsets in a tile's rows within 2 GiB; k is at least a piece
-bool tiled_linear_takes(const LinearArgs &a) { return a.K >= 16 && a.ldx <= (1 << 22) && a.ldw <= (1 << 22); }
-
 // Rows and weights that start at multiples of 16 bytes, with whole 16-byte pieces of k, are copied without a stop in registers
 static bool direct(const LinearArgs &a)
 {
@@ -451,7 +448,7 @@ static hipError_t launch_one(const LinearArgs &a, int splits, hipStream_t st)
     t.steps_per = (steps + splits - 1) / splits;
     t.splits = (steps + t.steps_per - 1) / t.steps_per;    // (no range without a step)
     t.counters = (unsigned *)a.workspace;
-    t.part = (int32_t *)((uint8_t *)a.workspace + kWsCounterBytes);
+    t.part = (int32_t *)((uint8_t *)a.workspace + kSplitCounterBytes);
     const long long units = (long long)t.tiles_n * t.tiles_m * t.splits, per = (units + 7) / 8;
     if (!fits_launch(per * 8, WN * WM * 64)) return hipErrorInvalidConfiguration;
     t.per_xcd = (int)per;
@@ -470,74 +467,10 @@ static hipError_t launch_tiles(const LinearArgs &a, int splits, hipStream_t st)
     return a.w2 ? launch_one<TN, TM, WN, WM, BK, 2, true, false>(a, splits, st) : launch_one<TN, TM, WN, WM, BK, 2, false, false>(a, splits, st);
 }
 
-// Which tile, and in how many ranges of k.  A tile's time is a part that does not depend on k (start, epilogue) and one for each 128 bytes of k; tiles beyond what
-// the 256 compute units hold at a time wait for another turn.  Measured in us: {rows, weight rows, held at a time, fixed, a step with few tiles on the chip, a
-// step with all}.
-struct TileCost {
-    int m, n, held;
-    float fixed, few, all;
-};
-constexpr TileCost kTiles[] = {
-    {256, 256, 256, 14.f, 1.15f, 1.75f},    // 4096 x 4096 -> 4096: 74 us (the next one: 79)
-    {128, 256, 256, 8.f, 0.55f, 1.f},       // gated 512 x 4096 -> 8192: 40 us (the one before 59, the next one 45)
-    {128, 128, 512, 6.f, 0.58f, 1.25f},     // two workgroups on a compute unit
-    {128, 128, 256, 8.5f, 0.48f, 0.58f},    // ... one, with four stages instead of two: 1024 x 4096 -> 4096: 26 us (the one before 35, the next one 30)
-    {64, 128, 512, 4.f, 0.29f, 0.75f},      // gated 77 x 2048 -> 5461: 9.4 us (the next one 10.2)
-    {64, 64, 512, 3.f, 0.22f, 0.46f},       // 128 x 4096 -> 4096: 10.2 us (the one before 13.9), 512 x 4096 -> 4096: 16.4 us (16.3); gated, by half the waves, 1.5 us more
-};
-constexpr int kTileKinds = sizeof(kTiles) / sizeof(kTiles[0]);
-constexpr int kMostSplits = 16, kSplitTiles = (int)(kWsCounterBytes / sizeof(unsigned));
-// us: the sums' way through memory and back, so much more for each range that one workgroup adds, and for each 64 x 64 sums that take it (64 x 16384 -> 512 in 64 x 64
-// tiles: whole 35 us, in 2, 4, 8, 16 ranges 20.9, 14.4, 12.6, 15.1; 512 x 4096 -> 4096 in two ranges of 64 x 128 tiles 23.8, whole 16.3)
-constexpr float kExchange = 0.5f, kExchangeRange = 0.55f, kExchangeSums = 0.006f;
-
-struct TilePlan {
-    int tile, splits;
-    float us;
-};
-
-static TilePlan plan_tiles(const LinearArgs &a, bool may_split)
+// (the cases in the order of kTiles)
+hipError_t launch_tiled_linear(const LinearArgs &a, const TilePlan &p, hipStream_t st)
 {
-    TilePlan best = {0, 1, 0.f};
-    const int steps = (a.K + 127) / 128;
-    const float step = step_factor(a);
-    for (int c = 0; c < kTileKinds; ++c) {
-        if (g_tuning.ff_kernel >= 4 && c != g_tuning.ff_kernel - 4) continue;
-        const TileCost &t = kTiles[c];
-        const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + t.n - 1) / t.n);
-        for (int s = 1; s <= kMostSplits; ++s) {
-            if (s > 1 && (!may_split || tiles > (float)kSplitTiles || tiles * (float)s > (float)t.held || 2 * s > steps)) break;
-            // (one workgroup on each unit: all of the chip, or, of the tiles that two share a unit, a quarter of the way there; through registers less of it, and
-            // all where any unit has two: 384 x 5461 -> 2048 in 64 x 64 tiles 0.36 us a step, 1000 x 5461 -> 2048 0.73)
-            const float units = tiles * (float)s, turns = __builtin_ceilf(units / (float)t.held), on = units < (float)t.held ? units / 256.f : (float)t.held / 256.f;
-            const float full = t.held == 256 ? on : step > 1.f ? (on > 1.f ? 1.f : 0.15f * on) : on < 1.f ? 0.25f * on : 0.25f + 0.75f * (on - 1.f), more = c == kTileKinds - 1 && a.w2 ? 1.5f : 0.f;
-            const float us = turns * (t.fixed + more + (float)((steps + s - 1) / s) * step * (t.few + (t.all - t.few) * full)) + (s > 1 ? kExchange + kExchangeRange * (float)s + kExchangeSums * units * (float)(t.m * t.n / 4096) : 0.f);
-            if (g_tuning.ff_split ? s == 1 || s <= g_tuning.ff_split : best.us == 0.f || us < best.us) best = {c, s, us};
-        }
-    }
-    return best;
-}
-
-// (no less than the weights take from memory: 8 x 4096 -> 16384 18.8 us, 8 x 8192 -> 8192, in two ranges of k, 21.1, gated 16 x 4096 -> 16384 31.7)
-float tiled_linear_us(const LinearArgs &a, bool may_split)
-{
-    const TilePlan p = plan_tiles(a, may_split);
-    const float flow = 3.f + 0.205f * (a.w2 ? 2.f : 1.f) * (float)a.N * (float)a.K * 1e-6f + (p.splits > 1 ? 3.f : 0.f);
-    return p.us > flow ? p.us : flow;
-}
-
-size_t tiled_linear_workspace(const LinearArgs &a)
-{
-    const TilePlan p = plan_tiles(a, true);
-    if (p.splits == 1) return 0;
-    const TileCost &t = kTiles[p.tile];
-    const size_t tiles = (size_t)((a.M + t.m - 1) / t.m) * (size_t)(((a.w2 ? 2ll : 1ll) * a.N + t.n - 1) / t.n);
-    return kWsCounterBytes + tiles * (size_t)p.splits * (size_t)(t.m * t.n) * 4;
-}
-
-hipError_t launch_tiled_linear(const LinearArgs &a, hipStream_t st)
-{
-    const TilePlan p = plan_tiles(a, a.workspace != nullptr);
+    static_assert(kTileKinds == 6 && kSplitCounterBytes == kWsCounterBytes, "a case a tile; counters as in the other workspaces");
     switch (p.tile) {
     case 0: return launch_tiles<2, 4, 4, 2, 128, 2>(a, p.splits, st);
     case 1: return launch_tiles<2, 2, 4, 2, 128, 3>(a, p.splits, st);

@@ -119,9 +119,6 @@ __global__ __launch_bounds__(64 * (KW > 4 ? KW : 4)) void linear_tokens_kernel(c
     }
 }
 
-// (eight rows: 4096 -> 16384 15.4 us, by the kernel for few rows 16.1; 8192 -> 8192 16.1 and 14.7)
-bool tokens_linear_takes(const LinearArgs &a) { return a.M <= 4 && a.K >= 16 && a.K <= 32768 && fits_launch(a.N, 256); }
-
 template <int MR, int C, int KW, int OUT>
 static void launch_tokens(const LinearArgs &a, hipStream_t st)
 {
