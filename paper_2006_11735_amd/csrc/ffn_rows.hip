@@ -12,25 +12,32 @@ constexpr float kLeast = 0x1p-120f;
 // Maximum of magnitudes as bit patterns: they are ordered as integers, and a NaN's is above every number's
 __device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
 
+// What brings a row's numbers to 8 bits: 127 / max|v| as a float32 and what its rounding has left of it.  A number that is exactly between two of the 8-bit ones (half
+// of the largest one is, at 63.5) has to stay there for its tie to go to the even one: by the first part alone one of ten such numbers went to its other side.
+struct Factor {
+    float most, rest;
+};
+
 // (factor for the numbers, scale of the row).  A row that holds NaN or an infinity, or whose squares do not add up to a finite sum: numbers 0, scale NaN.
-__device__ __forceinline__ void row_scale(float squares, uint32_t most, const RowsArgs &a, float *factor, float *scale)
+__device__ __forceinline__ void row_scale(float squares, uint32_t most, const RowsArgs &a, Factor *factor, float *scale)
 {
     const float m = __builtin_bit_cast(float, most);
+    *factor = {};
     if (most >= 0x7f800000u || !(squares < __builtin_huge_valf())) {
-        *factor = 0.f;
         *scale = __builtin_nanf("");
     } else if (m < kLeast) {
-        *factor = *scale = 0.f;
+        *scale = 0.f;
     } else {
-        *factor = 127.f / m;
+        factor->most = 127.f / m;
+        factor->rest = __builtin_fmaf(-factor->most, m, 127.f) * (factor->most * (1.f / 127.f));      // (what is left of 127, over m)
         *scale = m / 127.f * (a.gamma ? 1.f / sqrtf(squares / (float)a.c + a.eps) : 1.f);
     }
 }
 
 // one number in 8 bits; a factor of 0 makes any number 0
-__device__ __forceinline__ int to_byte(float v, float factor)
+__device__ __forceinline__ int to_byte(float v, const Factor &f)
 {
-    return factor == 0.f ? 0 : (int)rintf(v * factor);
+    return f.most == 0.f ? 0 : (int)rintf(__builtin_fmaf(v, f.most, v * f.rest));
 }
 
 // One workgroup a row, two passes over it.
@@ -61,7 +68,8 @@ __global__ __launch_bounds__(256) void rows_kernel(const RowsArgs a)
     __syncthreads();
     squares = (squares_of[0] + squares_of[1]) + (squares_of[2] + squares_of[3]);
     most = max(max(most_of[0], most_of[1]), max(most_of[2], most_of[3]));
-    float factor, scale;
+    Factor factor;
+    float scale;
     row_scale(squares, most, a, &factor, &scale);
     if (t == 0) a.scale[row] = scale;
     for (int i = t; i < a.c; i += 256) {
@@ -185,7 +193,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows_held_kernel(const Rows
             most = max(most, most_of[q]);
         }
     }
-    float factor, scale;
+    Factor factor;
+    float scale;
     row_scale(squares, most, a, &factor, &scale);
     if (t == 0) a.scale[row] = scale;
 #pragma unroll
