@@ -572,7 +572,8 @@ typedef enum {
  *   scale = max over c of |u| / 127
  *   q     = u / scale, to nearest, ties to even: in [-127, 127], the row's largest magnitude at 127
  * A row of zeros (largest |s * gamma|, or |x|, below 2^-120) has scale 0 and numbers 0.  A row that holds a NaN or an infinity, or numbers
- * whose squares or products with gamma leave float32, has scale NaN and numbers 0: each of its values is NaN.
+ * whose squares or products with gamma leave float32 upwards, has scale NaN and numbers 0: each of its values is NaN.  So are those of a row whose scale
+ * would leave float32, which is NaN.  Squares may leave float32 downwards.
  * gamma: c numbers of gamma_dtype (the stream's type or ICNN_F32).  scale: `rows` float32.  No output may overlap an input (but for `sum` as above) or
  * another output: ICNN_E_UNSUPPORTED.  iquantize_rows_s8 uses rows, c, x_stride, q_stride and dtype.
  */

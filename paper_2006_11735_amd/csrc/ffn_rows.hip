@@ -18,6 +18,47 @@ struct Factor {
     float most, rest;
 };
 
+// Below this the squares of a row may have been rounded as subnormal numbers or to zero: each is off by 2^-150 at most, 2^20 of them by 2^-130, which is
+// nothing beside a sum or an eps of 2^-100.  What is below is taken again, from memory, in 64 bits: rows of numbers of 1e-15 and less, with hardly any eps.
+constexpr float kLeastSquares = 0x1p-100f;
+
+__device__ __forceinline__ bool squares_are_lost(float squares, uint32_t most, const RowsArgs &a)
+{
+    return squares < kLeastSquares && a.eps < kLeastSquares && __builtin_bit_cast(float, most) >= kLeast;
+}
+
+// Number i of the row as the norm takes it, once more: its own thread asks, which has stored the sum where there is one (maybe over x or the residual)
+__device__ __forceinline__ float number_again(const RowsArgs &a, long long row, int i)
+{
+    if (a.sum) return load_number(a.sum, row * a.lds + i, a.dtype);
+    const float x = load_number(a.x, row * a.ldx + i, a.dtype);
+    return a.res ? round_number(x + load_number(a.res, row * a.ldr + i, a.dtype), a.dtype) : x;
+}
+
+// The sum over a row's threads, of one wave or of WAVES of them
+template <int WAVES>
+__device__ __forceinline__ double sum_of_row(double v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    if constexpr (WAVES > 1) {
+        __shared__ double part[WAVES];
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0;
+        for (int q = 0; q < WAVES; ++q) v += part[q];
+    }
+    return v;
+}
+
+// (a scale that would be infinite is NaN)
+__device__ __forceinline__ float finite_or_nan(float scale) { return scale < __builtin_huge_valf() ? scale : __builtin_nanf(""); }
+
+__device__ __forceinline__ float scale_of_wide(double squares, uint32_t most, const RowsArgs &a)
+{
+    return finite_or_nan((float)((double)__builtin_bit_cast(float, most) / 127 / sqrt(squares / a.c + (double)a.eps)));
+}
+
 // (factor for the numbers, scale of the row).  A row that holds NaN or an infinity, or whose squares do not add up to a finite sum: numbers 0, scale NaN.
 __device__ __forceinline__ void row_scale(float squares, uint32_t most, const RowsArgs &a, Factor *factor, float *scale)
 {
@@ -30,7 +71,7 @@ __device__ __forceinline__ void row_scale(float squares, uint32_t most, const Ro
     } else {
         factor->most = 127.f / m;
         factor->rest = __builtin_fmaf(-factor->most, m, 127.f) * (factor->most * (1.f / 127.f));      // (what is left of 127, over m)
-        *scale = m / 127.f * (a.gamma ? 1.f / sqrtf(squares / (float)a.c + a.eps) : 1.f);
+        *scale = finite_or_nan(m / 127.f * (a.gamma ? 1.f / sqrtf(squares / (float)a.c + a.eps) : 1.f));
     }
 }
 
@@ -83,6 +124,15 @@ __global__ __launch_bounds__(256) void rows_kernel(const RowsArgs a)
         if (a.gamma) s *= load_number(a.gamma, i, a.gamma_dtype);
         a.q[row * a.ldq + i] = (int8_t)to_byte(s, factor);
     }
+    if (a.gamma && squares_are_lost(squares, most, a)) {
+        double wide = 0;
+        for (int i = t; i < a.c; i += 256) {
+            const double s = number_again(a, row, i);
+            wide += s * s;
+        }
+        scale = scale_of_wide(sum_of_row<4>(wide), most, a);
+        if (t == 0) a.scale[row] = scale;
+    }
 }
 
 // Eight numbers of a stream that is read once
@@ -103,8 +153,8 @@ typedef int v2i_any __attribute__((ext_vector_type(2), aligned(1)));
 
 // Rows that fit a workgroup's registers: read once.  T threads a row (a wave, with neither LDS nor a barrier, or more), V times eight numbers a thread.  All loads of a
 // row are on their way before the first is waited for: they stay bits until then, since a conversion in the branch that has loaded would wait there.
-// DT: the stream's type; GT: gamma's, 0 = no norm.
-template <int DT, int GT, int T, int V>
+// DT: the stream's type; GT: gamma's, 0 = no norm; TINY: eps is so small that squares may be lost (1 x 4096 2.9 us, with the code for them 3.0).
+template <int DT, int GT, bool TINY, int T, int V>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rows_held_kernel(const RowsArgs a)
 {
     constexpr int WAVES = T / 64, GD = GT ? GT : kF32;
@@ -212,22 +262,40 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows_held_kernel(const Rows
                 if (i + e < a.c) at[e] = (int8_t)(b[e >> 2] >> (8 * (e & 3)));
         }
     }
+    if (TINY && squares_are_lost(squares, most, a)) {
+        double wide = 0;
+        for (int k = 0; k < V; ++k)
+            for (int i = 8 * (k * T + t), e = 0; e < 8 && i + e < a.c; ++e) {
+                const double s = number_again(a, row, i + e);
+                wide += s * s;
+            }
+        scale = scale_of_wide(sum_of_row<WAVES>(wide), most, a);
+        if (t == 0) a.scale[row] = scale;
+    }
+}
+
+template <int DT, int GT, bool TINY>
+static hipError_t launch_rows_held(const RowsArgs &a, hipStream_t st)
+{
+    const dim3 four((unsigned)((a.rows + 3) / 4)), one((unsigned)a.rows);
+    if (a.c <= 512) hipLaunchKernelGGL((rows_held_kernel<DT, GT, TINY, 64, 1>), four, dim3(256), 0, st, a);
+    else if (a.c <= 1024) hipLaunchKernelGGL((rows_held_kernel<DT, GT, TINY, 64, 2>), four, dim3(256), 0, st, a);
+    else if (a.c <= 2048) hipLaunchKernelGGL((rows_held_kernel<DT, GT, TINY, 256, 1>), one, dim3(256), 0, st, a);
+    else if (a.c <= 4096) hipLaunchKernelGGL((rows_held_kernel<DT, GT, TINY, 256, 2>), one, dim3(256), 0, st, a);
+    else if (a.c <= 6144) hipLaunchKernelGGL((rows_held_kernel<DT, GT, TINY, 256, 3>), one, dim3(256), 0, st, a);
+    else if (a.c <= 8192) hipLaunchKernelGGL((rows_held_kernel<DT, GT, TINY, 256, 4>), one, dim3(256), 0, st, a);
+    else if (a.c <= 16384) hipLaunchKernelGGL((rows_held_kernel<DT, GT, TINY, 512, 4>), one, dim3(512), 0, st, a);      // (by 1024 threads: 2048 x 16384 20.6 us instead of 18.7, 2048 x 11008 18.1 instead of 15)
+    else if (a.c <= 32768) hipLaunchKernelGGL((rows_held_kernel<DT, GT, TINY, 1024, 4>), one, dim3(1024), 0, st, a);
+    else hipLaunchKernelGGL(rows_kernel, one, dim3(256), 0, st, a);
+    return hipGetLastError();
 }
 
 template <int DT, int GT>
 static hipError_t launch_rows_of(const RowsArgs &a, hipStream_t st)
 {
-    const dim3 four((unsigned)((a.rows + 3) / 4)), one((unsigned)a.rows);
-    if (a.c <= 512) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 64, 1>), four, dim3(256), 0, st, a);
-    else if (a.c <= 1024) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 64, 2>), four, dim3(256), 0, st, a);
-    else if (a.c <= 2048) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 256, 1>), one, dim3(256), 0, st, a);
-    else if (a.c <= 4096) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 256, 2>), one, dim3(256), 0, st, a);
-    else if (a.c <= 6144) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 256, 3>), one, dim3(256), 0, st, a);
-    else if (a.c <= 8192) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 256, 4>), one, dim3(256), 0, st, a);
-    else if (a.c <= 16384) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 512, 4>), one, dim3(512), 0, st, a);      // (by 1024 threads: 2048 x 16384 20.6 us instead of 18.7, 2048 x 11008 18.1 instead of 15)
-    else if (a.c <= 32768) hipLaunchKernelGGL((rows_held_kernel<DT, GT, 1024, 4>), one, dim3(1024), 0, st, a);
-    else hipLaunchKernelGGL(rows_kernel, one, dim3(256), 0, st, a);
-    return hipGetLastError();
+    if constexpr (GT != 0)
+        if (a.eps < kLeastSquares) return launch_rows_held<DT, GT, true>(a, st);
+    return launch_rows_held<DT, GT, false>(a, st);
 }
 
 static hipError_t launch_some_rows(const RowsArgs &a, hipStream_t st)
