@@ -55,21 +55,33 @@ class FeedForward:
         self.q, self.q_scale = new((rows, width), torch.int8), new(rows, torch.float32)
         self.middle = new((rows, hidden), dtype)
         self.h, self.h_scale = new((rows, hidden), torch.int8), new(rows, torch.float32)
-        self._lists, self._workspace = {}, None
+        # One workspace for the calls of every row count, cleared here: a run's stream knows nothing of this one's, and what a captured run clears is cleared only when the
+        # graph is replayed.  A size is the same for all counts up to a multiple of 64, and up to 4, 8, 16 and 32.
+        counts = {min(c, rows) for c in (4, 8, 16, 32, *range(64, rows + 64, 64))}
+        size = max(self._workspace_bytes(*self._products(c)) for c in counts)
+        self._workspace = new(size, torch.uint8) if size else None
+        self._lists = {}
+        torch.cuda.synchronize(self.stream.device)             # what was cleared and quantised is there for runs on any stream
+
+    def _products(self, n):
+        """Descriptors of the products of n rows, up and down"""
+        code = _CODES[self.dtype]
+        return (B.linear_desc(rows=n, k=self.width, n=self.hidden, act=ACTS[self.act], dtype=code), B.linear_desc(rows=n, k=self.hidden, n=self.width, dtype=code))
+
+    def _workspace_bytes(self, up, down):
+        return max((B.ilinear_s8_workspace_bytes if self.weights[1] is None else B.igated_linear_s8_workspace_bytes)(up), B.ilinear_s8_workspace_bytes(down))
 
     def calls(self, n):
         """The block's four calls on the first n rows, as (kind, arguments)."""
         code = _CODES[self.dtype]
         norm = B.norm_desc(rows=n, c=self.width, dtype=code, gamma_dtype=B.ICNN_F32, eps=self.eps)
-        up = B.linear_desc(rows=n, k=self.width, n=self.hidden, act=ACTS[self.act], dtype=code)
+        up, down = self._products(n)
         rows = B.norm_desc(rows=n, c=self.hidden, dtype=code)
-        down = B.linear_desc(rows=n, k=self.hidden, n=self.width, dtype=code)
         (wg, sg), second, (wd, sd) = self.weights
         bg, bu, bd = self.biases
-        size = max((B.ilinear_s8_workspace_bytes if second is None else B.igated_linear_s8_workspace_bytes)(up), B.ilinear_s8_workspace_bytes(down))
-        if size and (self._workspace is None or self._workspace.numel() < size):       # (the lists made so far keep theirs)
-            self._workspace = torch.zeros(size, dtype=torch.uint8, device=self.stream.device)
-        ws = self._workspace if size else None
+        ws = self._workspace
+        if ws is not None and self._workspace_bytes(up, down) > ws.numel():            # (under another tuning than the constructor's: k stays whole)
+            ws = None
         if second is None:
             first = ("linear", (up, self.q, self.q_scale, wg, sg, bg, None, self.middle, ws))
         else:
