@@ -25,7 +25,8 @@ def quantize_weights(w):
     """(int8 [n][k], float32 [n]) of floating weights on the GPU: per output channel the step max|w| / 127 (Section 3.1, Section 3.4.3)."""
     n, k = w.shape
     q, step = torch.empty((n, k), dtype=torch.int8, device=w.device), torch.empty(n, dtype=torch.float32, device=w.device)
-    B.iquantize_rows_s8(B.norm_desc(rows=n, c=k, x_stride=w.stride(0), dtype=_CODES[w.dtype]), w, q, step)
+    with torch.cuda.device(w.device):
+        B.iquantize_rows_s8(B.norm_desc(rows=n, c=k, x_stride=w.stride(0), dtype=_CODES[w.dtype]), w, q, step)
     return q, step
 
 
@@ -96,7 +97,8 @@ class FeedForward:
             raise ValueError("%d rows: the buffers hold %d" % (n, self.rows))
         if n not in self._lists:
             self._lists[n] = B.Calls(self.calls(n))
-        self._lists[n].run(stream)
+        with torch.cuda.device(self.stream.device):            # (without a stream: torch's current one of this device)
+            self._lists[n].run(stream)
 
 
 def main():

@@ -79,3 +79,10 @@ def test_nothing_is_allocated_or_cleared_by_a_run(events, monkeypatch):
         ff.run(n, stream=7)
         assert events[-1][0] == "run"
     assert len({id(a[-1]) for e in events if e[0] == "run" for kind, a in e[2] if kind == "linear" and a[-1] is not None}) == 1
+
+
+def test_everything_is_issued_on_the_block_s_device(events):
+    """The stream that a call takes by itself is the current device's."""
+    ff = block(64, 128, 8)
+    ff.run(3)
+    assert [e[:2] for e in events if e[0] != "wait"] == [("quantize", torch.device("cpu"))] * 3 + [("run", torch.device("cpu"))]
