@@ -23,7 +23,11 @@ ACTS = {"none": B.ICNN_ACT_NONE, "relu": B.ICNN_ACT_RELU, "silu": B.ICNN_ACT_SIL
 
 def quantize_weights(w):
     """(int8 [n][k], float32 [n]) of floating weights on the GPU: per output channel the step max|w| / 127 (Section 3.1, Section 3.4.3)."""
+    if w.dim() != 2 or w.dtype not in _CODES:
+        raise ValueError("weights are [n][k] numbers of float32, float16 or bfloat16: got %s of %s" % (tuple(w.shape), w.dtype))
     n, k = w.shape
+    if w.stride(1) != 1 or w.stride(0) < k:                    # (the library takes rows whose numbers lie next to each other, and no two rows in one place)
+        w = w.contiguous()
     q, step = torch.empty((n, k), dtype=torch.int8, device=w.device), torch.empty(n, dtype=torch.float32, device=w.device)
     with torch.cuda.device(w.device):
         B.iquantize_rows_s8(B.norm_desc(rows=n, c=k, x_stride=w.stride(0), dtype=_CODES[w.dtype]), w, q, step)

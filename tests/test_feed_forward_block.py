@@ -86,3 +86,24 @@ def test_everything_is_issued_on_the_block_s_device(events):
     ff = block(64, 128, 8)
     ff.run(3)
     assert [e[:2] for e in events if e[0] != "wait"] == [("quantize", torch.device("cpu"))] * 3 + [("run", torch.device("cpu"))]
+
+
+@pytest.mark.parametrize("name", ["columns", "transposed", "rows", "one row", "one column", "broadcast rows", "offset"])
+def test_weights_are_quantised_from_their_own_numbers(events, monkeypatch, name):
+    w = torch.arange(24.0 * 40).reshape(24, 40)
+    w = {"columns": w[:, ::2], "transposed": w.t(), "rows": w[::3], "one row": w[3:4, ::4], "one column": w[:, 5:6], "broadcast rows": w[2].expand(6, 40),
+         "offset": w[1:, 3:30]}[name]
+    seen = []
+
+    def quantise(d, x, q, scale, stream=None):
+        seen.append(torch.as_strided(x, (d.rows, d.c), (d.x_stride, 1)).clone())
+        assert d.x_stride >= d.c and q.shape == w.shape and q.stride() == (d.c, 1) and scale.shape == (d.rows,)
+    monkeypatch.setattr(B, "iquantize_rows_s8", quantise)
+    ffn.quantize_weights(w)
+    assert torch.equal(seen[0], w)
+
+
+def test_weights_of_other_types_or_dimensions_are_refused(events):
+    for w in (torch.zeros(4, 4, dtype=torch.float64), torch.zeros(4, 4, dtype=torch.int8), torch.zeros(4), torch.zeros(2, 4, 4)):
+        with pytest.raises(ValueError):
+            ffn.quantize_weights(w)
