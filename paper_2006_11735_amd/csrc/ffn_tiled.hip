@@ -381,7 +381,7 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
             for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[8 * p + e] = (float)t[p][e >> 2][e & 3] * xs[p] * s1[e] + b1[e];
-            activate_all(v, a.act);
+            activate_all(v, a.act, DT);
             if (GATED) {
 #pragma unroll
                 for (int p = 0; p < P; ++p)

@@ -112,7 +112,7 @@ __global__ __launch_bounds__(64 * (KW > 4 ? KW : 4)) void linear_tokens_kernel(c
             if (GATED) c2 += part[wave + q][lane * L + 1];
         }
         float v[1] = {(float)c1 * xs * s1 + b1};
-        activate_all(v, a.act);
+        activate_all(v, a.act, a.dtype);
         if (GATED) v[0] *= (float)c2 * xs * s2 + b2;
         else if (a.res) v[0] += value_of(res, a.dtype);
         store_number(a.y, fm * a.ldy + fn, a.dtype, v[0]);
