@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void linear_plain_kernel(const LinearArgs a, i
     finish_four<GATED>(a, acc[0], acc[1], f, m, n0 + 4 * g);
 }
 
-hipError_t launch_linear(const LinearArgs &a, hipStream_t st)
+static hipError_t launch_range(const LinearArgs &a, hipStream_t st)
 {
     const LinearPlan plan = plan_launch(a, linear_tuning());
     switch (plan.kernel) {
@@ -54,10 +54,14 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t st)
     }
     const int tiles_n = (a.N + 15) / 16;
     const long long tiles = (long long)((a.M + 15) / 16) * tiles_n, blocks = (tiles + 3) / 4;
-    if (!fits_launch(blocks, 256)) return hipErrorInvalidConfiguration;
     if (a.w2) hipLaunchKernelGGL(linear_plain_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, a, tiles_n, tiles);
     else hipLaunchKernelGGL(linear_plain_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, a, tiles_n, tiles);
     return hipGetLastError();
+}
+
+hipError_t launch_linear(const LinearArgs &a, hipStream_t st)
+{
+    return each_range(a, a.dtype == kF32 ? 4 : 2, [&](const LinearArgs &b) { return launch_range(b, st); });
 }
 
 }  // namespace icnn

@@ -35,12 +35,12 @@ inline float step_factor(const LinearArgs &a)
 }
 
 // (eight rows: 4096 -> 16384 15.4 us, by the kernel for few rows 16.1; 8192 -> 8192 16.1 and 14.7)
-inline bool tokens_linear_takes(const LinearArgs &a) { return a.M <= 4 && a.K >= 16 && a.K <= 32768 && fits_launch(a.N, 256); }
+inline bool tokens_linear_takes(const LinearArgs &a) { return a.M <= 4 && a.K >= 16 && a.K <= 32768; }
 
 // The kernel for few rows: waves of a workgroup, bytes of a weight row that a wave takes a turn
 constexpr int kFewWaves = 4, kFewTurn = 256;
 // A tile's rows within 2 GiB of its first; k is at least a piece
-inline bool few_linear_takes(const LinearArgs &a) { return a.M <= 64 && a.K >= 16 && a.ldw <= (1 << 26) && fits_launch((a.N + 15) / 16, kFewWaves * 64); }
+inline bool few_linear_takes(const LinearArgs &a) { return a.M <= 64 && a.K >= 16 && a.ldw <= (1 << 26); }
 
 // Measured: a start, so much a megabyte of weights and so much for each time that the chip is filled with workgroups (each reads all rows; gated ones do it for
 // twice the weights), or a turn of a wave where few workgroups are on the chip (8 rows, 4096 -> 16384: 16.1 us, 8192 -> 8192: 14.7, gated 4096 -> 16384: 26.1; 16 rows,
@@ -151,10 +151,54 @@ inline size_t plan_workspace(const LinearArgs &a, const LinearPlan &p)
     return kSplitCounterBytes + tiles * (size_t)p.tiles.splits * (size_t)(t.m * t.n) * 4;
 }
 
+// A product whose outputs one launch might not hold goes in several: ranges of outputs n and, within, of rows.  As many as here fit by any kernel, on any rows and
+// weights: 16 x 16 outputs a wave (the plain kernel), 64 x 32 (the smallest gated tile) or 64 x 64 by at most 256 threads, one output by at most 512 (single tokens).
+constexpr long long kMostColumns = 1 << 22, kMostOutputs = 1ll << 33;
+static_assert(fits_launch(kMostOutputs / 1024 + 1, 256) && fits_launch(kMostOutputs / 2048 + 8, 256) && fits_launch(kMostColumns, 512), "any kernel's launch");
+
+inline long long rows_of_a_range(const LinearArgs &a)
+{
+    const long long columns = a.N < kMostColumns ? (a.N + 63ll) / 64 * 64 : kMostColumns;
+    return kMostOutputs / columns / 256 * 256;
+}
+
+inline bool one_range(const LinearArgs &a) { return a.N <= kMostColumns && a.M <= rows_of_a_range(a); }
+
+// fn of every range's operands, until it returns something.  `item`: bytes of an element of y.  Ranges of a larger product do not split k (they fill the chip; the last
+// ones need not).
+template <class F>
+inline auto each_range(const LinearArgs &a, int item, F &&fn) -> decltype(fn(a))
+{
+    if (one_range(a)) return fn(a);
+    const long long rows = rows_of_a_range(a);
+    for (long long n = 0; n < a.N; n += kMostColumns)
+        for (long long m = 0; m < a.M; m += rows) {
+            LinearArgs b = a;
+            b.M = (int)(a.M - m < rows ? a.M - m : rows);
+            b.N = (int)(a.N - n < kMostColumns ? a.N - n : kMostColumns);
+            b.x += m * a.ldx;
+            b.xs += m;
+            b.w += n * a.ldw;
+            b.ws += n;
+            if (a.bias) b.bias += n;
+            if (a.w2) {
+                b.w2 += n * a.ldw;
+                b.ws2 += n;
+            }
+            if (a.bias2) b.bias2 += n;
+            if (a.res) b.res = (const int8_t *)a.res + (m * a.ldr + n) * item;
+            b.y = (int8_t *)a.y + (m * a.ldy + n) * item;
+            b.workspace = nullptr;
+            if (auto e = fn(b)) return e;
+        }
+    return {};
+}
+
 // Bytes that a caller is asked for, who may put the operands anywhere afterwards: the most that plan_launch comes to at any addresses.  They can but raise the
 // step's factor above that of the strides and k, which `a` has here with operands at multiples of 16.
 inline size_t linear_workspace(const LinearArgs &a, const LinearTuning &tuning)
 {
+    if (!one_range(a)) return 0;
     size_t most = 0;
     for (float step : kStepFactors) {
         if (step < step_factor(a)) continue;

@@ -450,7 +450,6 @@ static hipError_t launch_one(const LinearArgs &a, int splits, hipStream_t st)
     t.counters = (unsigned *)a.workspace;
     t.part = (int32_t *)((uint8_t *)a.workspace + kSplitCounterBytes);
     const long long units = (long long)t.tiles_n * t.tiles_m * t.splits, per = (units + 7) / 8;
-    if (!fits_launch(per * 8, WN * WM * 64)) return hipErrorInvalidConfiguration;
     t.per_xcd = (int)per;
     auto *const k = linear_tiled_kernel<TN, TM, WN, WM, BK, STAGES, GATED, DIRECT>;
     if (LDS > 65536)

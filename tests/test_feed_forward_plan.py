@@ -13,10 +13,15 @@ AT = 1 << 24                                           # an address at a multipl
 
 
 @pytest.fixture(scope="module")
-def launch(tmp_path_factory):
-    lib = tmp_path_factory.mktemp("plan") / "ff_plan.so"
-    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-o", str(lib), os.path.join(HERE, "ff_plan.cpp")], check=True)
-    fn = ctypes.CDLL(str(lib)).ff_launch
+def lib(tmp_path_factory):
+    path = tmp_path_factory.mktemp("plan") / "ff_plan.so"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-o", str(path), os.path.join(HERE, "ff_plan.cpp")], check=True)
+    return ctypes.CDLL(str(path))
+
+
+@pytest.fixture(scope="module")
+def launch(lib):
+    fn = lib.ff_launch
     fn.argtypes = [ctypes.POINTER(ctypes.c_longlong), ctypes.c_int, *[ctypes.c_size_t] * 3, *[ctypes.c_int] * 3, ctypes.POINTER(ctypes.c_ulonglong)]
     fn.restype = None
 
@@ -73,3 +78,52 @@ def test_nor_under_a_tuning(launch, kernel, split):
 def test_the_sweep_reaches_launches_whose_plan_the_addresses_change(launch):
     plans = {tuple(launch(8, 11008, 1024, 0, x=x).values()) for x in (0, 1, 8)}
     assert len(plans) > 1 and any(p[2] > 1 for p in plans)
+
+
+MOST = (1 << 31) - (1 << 16)                           # rows or outputs of a descriptor
+
+
+def largest(lib, rows, k, n, gated, kernel=0):
+    """(launches of a product, threads of the largest, its kernel)"""
+    out = (ctypes.c_ulonglong * 3)()
+    lib.ff_launches((ctypes.c_longlong * 5)(rows, k, n, k, k), gated, kernel, out)
+    return tuple(out)
+
+
+@pytest.mark.parametrize("gated", [0, 1])
+@pytest.mark.parametrize("k", [1, 8, 16, 64, 1000, 8192, 16384, 40000])
+def test_every_launch_fits(lib, k, gated):
+    """fewer than 2^32 threads, whatever the sizes that a descriptor may have"""
+    sizes = [1, 5, 64, 65, 300, 1 << 13, (1 << 20) + 1, (1 << 22) + 1, 1 << 23, 1 << 24, 1 << 28, 1 << 30, MOST]
+    for rows, n in itertools.product(sizes, sizes):
+        if rows * n <= 1 << 38:                        # (half a terabyte of results)
+            count, threads, kernel = largest(lib, rows, k, n, gated)
+            assert count >= 1 and threads < 1 << 32, (rows, n, count, threads, kernel)
+            if rows * n <= 1 << 32 and n <= 1 << 22 and rows <= 1 << 26:
+                assert count == 1, (rows, n)
+            for forced in range(1, 10):
+                assert largest(lib, rows, k, n, gated, forced)[1] < 1 << 32, (rows, n, forced)
+
+
+@pytest.mark.parametrize("gated", [0, 1])
+@pytest.mark.parametrize("rows,n", [(1, 1), (300, 5000), (MOST, 1), (1, MOST), (MOST, 65), ((1 << 27) + 300, 64), (3, (1 << 22) + 1), (1 << 18, 1 << 18), (100001, (1 << 22) + 70000)])
+def test_ranges_cover_a_product_once(lib, rows, n, gated):
+    out = (ctypes.c_longlong * 4096)()
+    count = lib.ff_ranges((ctypes.c_longlong * 5)(rows, 16, n, 17, 19), gated, 1024, out)
+    assert count >= 1
+    parts = [tuple(out[4 * i:4 * i + 4]) for i in range(count)]
+    assert sum(m * w for _, m, _, w in parts) == rows * n and all(m > 0 and w > 0 and m0 + m <= rows and n0 + w <= n for m0, m, n0, w in parts)
+    columns = sorted({(n0, w) for _, _, n0, w in parts})
+    lines = sorted({(m0, m) for m0, m, _, _ in parts})
+    assert len(set(parts)) == count == len(columns) * len(lines)
+    for spans, end in ((columns, n), (lines, rows)):
+        at = 0
+        for first, size in spans:
+            assert first == at
+            at += size
+        assert at == end
+
+
+def test_a_product_in_several_launches_asks_for_no_workspace():
+    for rows, n in (((1 << 27) + 64, 64), (40, (1 << 22) + 64)):
+        assert asked(rows, 16384, n, 0) == 0 and asked(rows, 16384, n, 1) == 0
