@@ -601,7 +601,8 @@ int iquantize_rows_s8(const icnn_norm_desc *desc, const void *x, void *q, float 
  * workspace: at least ..._workspace_bytes bytes, 16-byte aligned, zero-filled once by the caller after allocating it (its first 4096 bytes are
  * counters that every call leaves at zero).  Products of few outputs and a long k want one, for the sums of a k axis that is split over workgroups; others ask for
  * 0 bytes.  NULL is taken everywhere: k stays whole then, with the same result.  One workspace of the largest size may serve all calls that run one after the other
- * on a stream; calls that may overlap in time need one each.  The size holds wherever the operands lie, and is that of the tuning in force.
+ * on a stream; calls that may overlap in time need one each.  The size holds wherever the operands lie, for calls under the tuning that it was asked under (a call
+ * under another one needs that one's size).
  */
 typedef struct {
     int64_t rows;                  /* 0 <= rows <= 2^31 - 2^16                     */

@@ -25,8 +25,8 @@ struct LinearTuning {
 // A launch holds fewer than 2^32 threads
 constexpr bool fits_launch(long long groups, int threads) { return groups <= 0xffffffffLL / threads; }
 
-// How much longer a step along k is where rows go through registers: 64 x 5456 -> 2048 (rows at multiples of 16) 15.2 us, 5464 (of 8) 15.9, 5461 19.7; 4096 x 2048 ->
-// 8192 in 256 x 256 tiles 86 us, 2047 115
+// How much longer a step along k is where rows go through registers: with k whole 64 x 5456 -> 2048 (rows at multiples of 16) 15.2 us,
+// 5464 (of 8) 15.8, 5461 19.8; 4096 x 2048 -> 8192 in 256 x 256 tiles 87 us, 2047 112
 constexpr float kStepFactors[] = {1.f, 1.2f, 1.7f};         // rows at multiples of 16 bytes, of 4, anywhere
 inline float step_factor(const LinearArgs &a)
 {
@@ -43,8 +43,8 @@ constexpr int kFewWaves = 4, kFewTurn = 256;
 inline bool few_linear_takes(const LinearArgs &a) { return a.M <= 64 && a.K >= 16 && a.ldw <= (1 << 26); }
 
 // Measured: a start, so much a megabyte of weights and so much for each time that the chip is filled with workgroups (each reads all rows; gated ones do it for
-// twice the weights), or a turn of a wave where few workgroups are on the chip (8 rows, 4096 -> 16384: 16.1 us, 8192 -> 8192: 14.7, gated 4096 -> 16384: 26.1; 16 rows,
-// 4096 -> 4096: 7.4, 1024 -> 16384: 9.0; 32 rows, 16384 -> 4096: 23, 4096 -> 16384: 27.7; 64 rows, 4096 -> 4096: 13.5, 16384 -> 512: 35)
+// twice the weights), or a turn of a wave where few workgroups are on the chip (8 rows, 4096 -> 16384: 16.5 us, 8192 -> 8192: 14.7, gated 4096 -> 16384: 26.6; 16 rows,
+// 4096 -> 4096: 7.6, 1024 -> 16384: 9.1; 32 rows, 16384 -> 4096: 23, 4096 -> 16384: 27.8; 64 rows, 4096 -> 4096: 14.4, 16384 -> 512: 35)
 inline float few_linear_us(const LinearArgs &a, float step)
 {
     const float mb = (a.w2 ? 2.f : 1.f) * (float)a.N * (float)a.K * 1e-6f, turns = (float)((a.K + kFewWaves * kFewTurn - 1) / (kFewWaves * kFewTurn));
@@ -70,17 +70,17 @@ struct TileCost {
     float fixed, few, all;
 };
 constexpr TileCost kTiles[] = {
-    {256, 256, 256, 14.f, 1.15f, 1.75f},    // 4096 x 4096 -> 4096: 74 us (the next one: 79)
+    {256, 256, 256, 14.f, 1.15f, 1.75f},    // 4096 x 4096 -> 4096: 72 us (the next one: 78)
     {128, 256, 256, 8.f, 0.55f, 1.f},       // gated 512 x 4096 -> 8192: 40 us (the one before 59, the next one 45)
     {128, 128, 512, 6.f, 0.58f, 1.25f},     // two workgroups on a compute unit
-    {128, 128, 256, 8.5f, 0.48f, 0.58f},    // ... one, with four stages instead of two: 1024 x 4096 -> 4096: 26 us (the one before 35, the next one 30)
-    {64, 128, 512, 4.f, 0.29f, 0.75f},      // gated 77 x 2048 -> 5461: 9.4 us (the next one 10.2)
-    {64, 64, 512, 3.f, 0.22f, 0.46f},       // 128 x 4096 -> 4096: 10.2 us (the one before 13.9), 512 x 4096 -> 4096: 16.4 us (16.3); gated, by half the waves, 1.5 us more
+    {128, 128, 256, 8.5f, 0.48f, 0.58f},    // ... one, with four stages instead of two: 1024 x 4096 -> 4096: 25 us (the one before 34, the next one 27)
+    {64, 128, 512, 4.f, 0.29f, 0.75f},      // gated 77 x 2048 -> 5461: 10.1 us (the next one 11.1), -> 5456: 9.3 (10.2)
+    {64, 64, 512, 3.f, 0.22f, 0.46f},       // 128 x 4096 -> 4096: 9.2 us (the one before 10.8), 512 x 4096 -> 4096: 15.9 us (15.7); gated, by half the waves, 1.5 us more
 };
 constexpr int kTileKinds = sizeof(kTiles) / sizeof(kTiles[0]);
 constexpr int kMostSplits = 16, kSplitTiles = (int)(kSplitCounterBytes / sizeof(unsigned));
 // us: the sums' way through memory and back, so much more for each range that one workgroup adds, and for each 64 x 64 sums that take it (64 x 16384 -> 512 in 64 x 64
-// tiles: whole 35 us, in 2, 4, 8, 16 ranges 20.9, 14.4, 12.6, 15.1; 512 x 4096 -> 4096 in two ranges of 64 x 128 tiles 23.8, whole 16.3)
+// tiles: whole 28.3 us, in 2, 4, 8, 16 ranges 17.5, 12.0, 10.5, 12.5; 512 x 4096 -> 4096 in two ranges of 64 x 128 tiles 23.6, whole 15.7)
 constexpr float kExchange = 0.5f, kExchangeRange = 0.55f, kExchangeSums = 0.006f;
 
 struct TilePlan {
@@ -109,14 +109,15 @@ inline TilePlan plan_tiles(const LinearArgs &a, const LinearTuning &tuning, floa
     return best;
 }
 
-// (no less than the weights take from memory: 8 x 4096 -> 16384 18.8 us, 8 x 8192 -> 8192, in two ranges of k, 21.1, gated 16 x 4096 -> 16384 31.7)
+// (no less than the weights take from memory: 8 x 4096 -> 16384 18.8 us, 8 x 8192 -> 8192, in two ranges of k, 21.1, gated 16 x 4096 -> 16384 31.7, which the
+// kernel for few rows has in 28.3)
 inline float tiled_linear_us(const LinearArgs &a, const TilePlan &p)
 {
     const float flow = 3.f + 0.205f * (a.w2 ? 2.f : 1.f) * (float)a.N * (float)a.K * 1e-6f + (p.splits > 1 ? 3.f : 0.f);
     return p.us > flow ? p.us : flow;
 }
 
-// Up to four rows go token by token (1 x 16384 -> 4096: 12.3 us, by the kernel for few rows 16.1; 4 rows: 14.0 and 16.4), the others where they take least by what
+// Up to four rows go token by token (1 x 16384 -> 4096: 12.4 us, by the kernel for few rows 17.6; 4 rows: 14.1 and 16.4), the others where they take least by what
 // has been measured; what none of those takes (k below 16, rows gigabytes apart) by the plain kernel.
 enum class LinearKernel { plain, tokens, few, tiled };
 struct LinearPlan {

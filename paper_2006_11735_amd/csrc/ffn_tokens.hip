@@ -1,7 +1,7 @@
 // Products of up to four 8-bit rows and weights (see ffn_linear.hip for the mathematics): the single tokens of a decoder.  Nothing but the weights' way from memory
 // counts.  A wave reads whole kilobytes of a weight row an instruction (16 bytes a lane), all of its rows' in flight at once, against the rows' pieces that it
 // keeps in registers; sums are taken four products an instruction (v_dot4) and joined over the lanes at the end, over the KW waves that share the k axis in LDS.
-// 1 x 16384 -> 4096: 12.3 us (5.5 TB/s), 1 x 4096 -> 16384: 11.7, gated 1 x 4096 -> 16384: 21.3 (6.3 TB/s); 4 rows: 14.0, 12.9 and 22.0.
+// 1 x 16384 -> 4096: 12.4 us (5.4 TB/s), 1 x 4096 -> 16384: 11.9, gated 1 x 4096 -> 16384: 21.3 (6.3 TB/s); 4 rows: 14.1, 13.1 and 22.2.
 #include "ffn_common.h"
 
 namespace icnn {
