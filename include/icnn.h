@@ -466,7 +466,9 @@ typedef enum {
     ICNN_CALL_BOTTLENECK_DUAL = 6, ICNN_CALL_PAIR = 7, ICNN_CALL_TWIN = 8, ICNN_CALL_CHAIN = 9, ICNN_CALL_MAXPOOL = 10, ICNN_CALL_AVGPOOL = 11,
     ICNN_CALL_CONV_MAXPOOL_PC = 12, ICNN_CALL_BOTTLENECK_PC = 13, ICNN_CALL_BOTTLENECK_DUAL_PC = 14, ICNN_CALL_PAIR_PC = 15,
     ICNN_CALL_TWIN_LAST = 16, ICNN_CALL_TRIPLE = 17, ICNN_CALL_TRIPLE_PC = 18,
-    ICNN_CALL_RMS_NORM = 19, ICNN_CALL_QUANTIZE_ROWS = 20, ICNN_CALL_LINEAR = 21, ICNN_CALL_GATED_LINEAR = 22
+    ICNN_CALL_RMS_NORM = 19, ICNN_CALL_QUANTIZE_ROWS = 20, ICNN_CALL_LINEAR = 21, ICNN_CALL_GATED_LINEAR = 22,
+    ICNN_CALL_ROUTE = 23, ICNN_CALL_COMBINE = 24, ICNN_CALL_GROUPED_LINEAR = 25, ICNN_CALL_GROUPED_GATED_LINEAR = 26, ICNN_CALL_LINEAR_S4 = 27,
+    ICNN_CALL_GATED_LINEAR_S4 = 28
 } icnn_call_kind;
 typedef struct {
     int32_t kind;                  /* icnn_call_kind */
@@ -620,6 +622,125 @@ int ilinear_s8(const icnn_linear_desc *desc, const void *x, const float *x_scale
 int igated_linear_s8_workspace_bytes(const icnn_linear_desc *desc, size_t *bytes);
 int igated_linear_s8(const icnn_linear_desc *desc, const void *x, const float *x_scale, const void *w_gate, const float *gate_scale,
                      const float *gate_bias, const void *w_up, const float *up_scale, const float *up_bias, void *y, void *workspace, void *stream);
+
+/*
+ * The feed-forward half with experts: each token's row goes through the layers of the few experts that a router picks for it.
+ *
+ *   iroute_top                 the router's logits -> a token's experts and gates, and all tokens' positions in the order of their experts
+ *   igrouped_gated_linear_s8   hidden = act(q Wg_e) * (q Wu_e), e a position's expert; q's rows read where the tokens have them
+ *   iquantize_rows_s8          q, scale = rows of hidden in 8 bits
+ *   igrouped_linear_s8         v = act(q W_e)
+ *   icombine_rows              stream = residual + the sum of a token's rows of v by its gates
+ *
+ * Positions are on the device alone: no call waits for their number, and all take the capacity rows * top.
+ */
+
+/*
+ * The router.  A token's choices are its `top` largest logits in descending order; of equal ones that with the lowest index comes first.  Minus infinity is
+ * never chosen; a NaN is above every number.
+ *   expert[t][j]   the expert of choice j, -1 where fewer than j + 1 could be chosen
+ *   gate[t][j]     ICNN_ROUTE_SOFTMAX: scale * exp(l_j - max) / sum over all experts of exp(l - max);  ICNN_ROUTE_SIGMOID: scale / (1 + exp(-l_j));
+ *                  normalise: the sum is over the chosen ones, and the sigmoids are divided by theirs.  0 where there is no expert
+ *   place[t][j]    the choice's position: choices lie in the order of their experts, those of one expert in the order of their tokens; -1 where there is no expert
+ *   token[i]       the token of position i, -1 for the positions behind the last (offsets[experts] and up)
+ *   offsets[e]     expert e's positions are offsets[e] .. offsets[e + 1] - 1: experts + 1 numbers, offsets[0] = 0
+ * expert, gate and place are [rows][top], token has rows * top numbers.  With no rows the offsets are zeros and nothing else is read or written.
+ * workspace: iroute_top_workspace_bytes bytes, 16-byte aligned, of any contents (NULL where that is 0); calls that may overlap in time need one each.
+ * No output may overlap another, the workspace or the logits: ICNN_E_UNSUPPORTED.
+ */
+typedef enum { ICNN_ROUTE_SOFTMAX = 0, ICNN_ROUTE_SIGMOID = 1 } icnn_route_score;
+typedef struct {
+    int64_t rows;                  /* 0 <= rows * top <= 2^31 - 2^16               */
+    int64_t logits_stride;         /* >= experts                                   */
+    int32_t experts, top;          /* 1 <= experts <= 1024, 1 <= top <= 16, top <= experts */
+    int32_t dtype;                 /* of the logits: ICNN_F32, F16 or BF16         */
+    int32_t score;                 /* icnn_route_score                             */
+    int32_t normalise;             /* 0 or 1                                       */
+    float scale;                   /* finite                                       */
+} icnn_route_desc;
+
+int iroute_top_workspace_bytes(const icnn_route_desc *desc, size_t *bytes);
+int iroute_top(const icnn_route_desc *desc, const void *logits, int32_t *expert, float *gate, int32_t *place, int32_t *token, int32_t *offsets, void *workspace,
+               void *stream);
+
+/*
+ * Products grouped by expert: position i of expert e (offsets[e] <= i < offsets[e + 1]), r = index[i] (index NULL: r = i),
+ *   v[i][n] = act(sum over k of x[r][k] * w[e][n][k] * x_scale[r] * w_scale[e][n] + bias[e][n])
+ *   igrouped_linear_s8:        y = v
+ *   igrouped_gated_linear_s8:  y = v * (the same of w_up, up_scale and up_bias, without act);   v of w_gate, gate_scale, gate_bias
+ * with x, scales, biases, sums and y as in ilinear_s8: sums are exact, so a position's row does not depend on what else is in the call.  Scales and biases are
+ * [experts][n].  Rows of y that belong to no expert (in front of offsets[0], behind offsets[experts], and those whose index is not in [0, x_rows)) are left as they
+ * were.  Offsets have to ascend; of others only so much holds that nothing but y's rows is written and nothing outside the operands is read.
+ * y may not overlap another operand: ICNN_E_UNSUPPORTED.  (rows / 16 + min(rows, experts)) * ceil(n / 16) is at most 2^25.
+ */
+typedef struct {
+    int64_t rows;                  /* positions, y's rows: 0 <= rows <= 2^31 - 2^16 */
+    int64_t x_rows;                /* rows of x; without an index at least `rows`  */
+    int64_t x_stride, w_stride;    /* >= k                                         */
+    int64_t expert_stride;         /* from one expert's weights to the next: >= (n - 1) * w_stride + k */
+    int64_t y_stride;              /* >= n                                         */
+    int32_t k, n;                  /* 1 <= k <= 131071, 1 <= n <= 2^22             */
+    int32_t experts;               /* 1 <= experts <= 1024                         */
+    int32_t act;                   /* icnn_act                                     */
+    int32_t dtype;                 /* of y: ICNN_F32, F16 or BF16                  */
+} icnn_grouped_desc;
+
+int igrouped_linear_s8(const icnn_grouped_desc *desc, const void *x, const float *x_scale, const int32_t *index, const int32_t *offsets, const void *w,
+                       const float *w_scale, const float *bias, void *y, void *stream);
+int igrouped_gated_linear_s8(const icnn_grouped_desc *desc, const void *x, const float *x_scale, const int32_t *index, const int32_t *offsets, const void *w_gate,
+                             const float *gate_scale, const float *gate_bias, const void *w_up, const float *up_scale, const float *up_bias, void *y, void *stream);
+
+/*
+ * The sum of a token's rows: y[t] = residual[t] + sum over j of gate[t][j] * v[place[t][j]]   (residual NULL: none; it may be y itself)
+ * in float32, rounded once.  A choice whose place is not in [0, v_rows) adds nothing.  y may not overlap another operand but its residual in place.
+ */
+typedef struct {
+    int64_t rows, v_rows;          /* 0 <= rows * top, v_rows <= 2^31 - 2^16       */
+    int64_t v_stride, res_stride, y_stride;   /* >= c                              */
+    int32_t top, c;                /* 1 <= top <= 16, 1 <= c <= 2^20               */
+    int32_t dtype;                 /* of residual and y: ICNN_F32, F16 or BF16     */
+    int32_t v_dtype;               /* of v, likewise                               */
+} icnn_combine_desc;
+
+int icombine_rows(const icnn_combine_desc *desc, const void *v, const float *gate, const int32_t *place, const void *residual, void *y, void *stream);
+
+/*
+ * Products of 8-bit rows and 4-bit weights, two's complement, with a scale for each `group` numbers of a row:
+ *   v[m][n] = act(x_scale[m] * sum over groups g of w_scale[n][g] * (sum over the numbers k of g of x[m][k] * w[n][k]) + bias[n])
+ *   ilinear_s4:        y = v + residual[m][n]                                   (residual NULL: none; it may be y itself)
+ *   igated_linear_s4:  y = v * (the same of up_packed, up_scale and up_bias, without act);   v of gate_packed, gate_scale, gate_bias
+ * A group's sum is exact (int32); the sum over the groups is in float32, in an order that depends on the number of rows and on the sizes: the same row in calls of other
+ * row counts may differ in its last bits.
+ * Packed weights: iweights_s4_bytes bytes, 16-byte aligned; row n is ceil(k / 32) blocks of 16 bytes, byte j of a block holds number 32 b + j in its lower and number
+ * 32 b + 16 + j in its upper four bits; what is behind k may be anything.  w_scale: scale_dtype [n][ceil(k / group)].
+ * y may not overlap another operand but its residual in place.  ceil(rows / 16) * ceil(n / 16) is at most 2^25.
+ *
+ * iquantize_weights_s4 makes both of floating weights, once: scale = max|w| / 7 of a group, rounded to its type; number = w / scale to nearest, ties to even,
+ * in [-7, 7].  A group of zeros, or whose scale is rounded to zero, has scale 0 and numbers 0; one that holds a NaN or an infinity, or whose scale leaves its type, scale
+ * NaN and numbers 0.
+ */
+typedef struct {
+    int64_t rows;                  /* 0 <= rows <= 2^31 - 2^16                     */
+    int64_t x_stride;              /* >= k                                         */
+    int64_t res_stride, y_stride;  /* >= n                                         */
+    int32_t k, n;                  /* 1 <= k <= 131071, 1 <= n <= 2^22             */
+    int32_t group;                 /* 32, 64, 128 or 256                           */
+    int32_t act;                   /* icnn_act                                     */
+    int32_t dtype;                 /* of y and residual: ICNN_F32, F16 or BF16     */
+    int32_t scale_dtype;           /* of the weights' scales, likewise             */
+} icnn_linear_s4_desc;
+typedef struct {
+    int64_t w_stride;              /* >= k                                         */
+    int32_t n, k, group;
+    int32_t dtype, scale_dtype;    /* of w, of its scales                          */
+} icnn_quantize_s4_desc;
+
+int iweights_s4_bytes(int32_t n, int32_t k, size_t *bytes);
+int iquantize_weights_s4(const icnn_quantize_s4_desc *desc, const void *w, void *w_packed, void *w_scale, void *stream);
+int ilinear_s4(const icnn_linear_s4_desc *desc, const void *x, const float *x_scale, const void *w_packed, const void *w_scale, const float *bias,
+               const void *residual, void *y, void *stream);
+int igated_linear_s4(const icnn_linear_s4_desc *desc, const void *x, const float *x_scale, const void *gate_packed, const void *gate_scale, const float *gate_bias,
+                     const void *up_packed, const void *up_scale, const float *up_bias, void *y, void *stream);
 
 /*
  * Measurement aids: the two roofs a convolution layer is judged against, as they are on the machine at hand

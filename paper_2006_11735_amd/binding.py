@@ -16,6 +16,7 @@ ICNN_IN_U8_LE127, ICNN_IN_S8, ICNN_IN_U8_FULL = 0, 1, 2
 ICNN_E_NULL, ICNN_E_SHAPE, ICNN_E_PARAM, ICNN_E_ALIGN, ICNN_E_UNSUPPORTED, ICNN_E_LAUNCH = -1, -2, -3, -4, -5, -6
 ICNN_U8, ICNN_S8, ICNN_S32, ICNN_F32, ICNN_F16, ICNN_BF16 = range(6)
 ICNN_ACT_NONE, ICNN_ACT_RELU, ICNN_ACT_SILU, ICNN_ACT_GELU, ICNN_ACT_GELU_TANH = range(5)
+ICNN_ROUTE_SOFTMAX, ICNN_ROUTE_SIGMOID = range(2)
 ICNN_OUT_BRELU_U8, ICNN_OUT_CLAMP_U8, ICNN_OUT_LINEAR_S8, ICNN_OUT_RAW_S32 = 0, 1, 2, 3
 ICNN_RES_NONE, ICNN_RES_PRE, ICNN_RES_POST = 0, 1, 2
 
@@ -48,6 +49,29 @@ class icnn_linear_desc(C.Structure):
         (k, C.c_int32) for k in ("k", "n", "act", "dtype")]
 
 
+class icnn_route_desc(C.Structure):
+    _fields_ = [(k, C.c_int64) for k in ("rows", "logits_stride")] + [(k, C.c_int32) for k in ("experts", "top", "dtype", "score", "normalise")] + [
+        ("scale", C.c_float)]
+
+
+class icnn_grouped_desc(C.Structure):
+    _fields_ = [(k, C.c_int64) for k in ("rows", "x_rows", "x_stride", "w_stride", "expert_stride", "y_stride")] + [
+        (k, C.c_int32) for k in ("k", "n", "experts", "act", "dtype")]
+
+
+class icnn_combine_desc(C.Structure):
+    _fields_ = [(k, C.c_int64) for k in ("rows", "v_rows", "v_stride", "res_stride", "y_stride")] + [(k, C.c_int32) for k in ("top", "c", "dtype", "v_dtype")]
+
+
+class icnn_linear_s4_desc(C.Structure):
+    _fields_ = [(k, C.c_int64) for k in ("rows", "x_stride", "res_stride", "y_stride")] + [
+        (k, C.c_int32) for k in ("k", "n", "group", "act", "dtype", "scale_dtype")]
+
+
+class icnn_quantize_s4_desc(C.Structure):
+    _fields_ = [("w_stride", C.c_int64)] + [(k, C.c_int32) for k in ("n", "k", "group", "dtype", "scale_dtype")]
+
+
 class icnn_call(C.Structure):
     _fields_ = [("kind", C.c_int32), ("i", C.c_int32 * 7), ("d", C.POINTER(icnn_conv_desc) * 4), ("p", C.c_void_p * 13),
                 ("list", C.c_void_p * 3)]
@@ -56,7 +80,8 @@ class icnn_call(C.Structure):
 (ICNN_CALL_CONV, ICNN_CALL_CONV_PC, ICNN_CALL_DUAL, ICNN_CALL_DUAL_PC, ICNN_CALL_CONV_MAXPOOL, ICNN_CALL_BOTTLENECK, ICNN_CALL_BOTTLENECK_DUAL,
  ICNN_CALL_PAIR, ICNN_CALL_TWIN, ICNN_CALL_CHAIN, ICNN_CALL_MAXPOOL, ICNN_CALL_AVGPOOL, ICNN_CALL_CONV_MAXPOOL_PC, ICNN_CALL_BOTTLENECK_PC,
  ICNN_CALL_BOTTLENECK_DUAL_PC, ICNN_CALL_PAIR_PC, ICNN_CALL_TWIN_LAST, ICNN_CALL_TRIPLE, ICNN_CALL_TRIPLE_PC,
- ICNN_CALL_RMS_NORM, ICNN_CALL_QUANTIZE_ROWS, ICNN_CALL_LINEAR, ICNN_CALL_GATED_LINEAR) = range(23)
+ ICNN_CALL_RMS_NORM, ICNN_CALL_QUANTIZE_ROWS, ICNN_CALL_LINEAR, ICNN_CALL_GATED_LINEAR, ICNN_CALL_ROUTE, ICNN_CALL_COMBINE, ICNN_CALL_GROUPED_LINEAR,
+ ICNN_CALL_GROUPED_GATED_LINEAR, ICNN_CALL_LINEAR_S4, ICNN_CALL_GATED_LINEAR_S4) = range(29)
 
 
 class IcnnError(RuntimeError):
@@ -121,6 +146,16 @@ _lib.iquantize_rows_s8.argtypes = [_normp] + [_vp] * 4
 _lib.ilinear_s8_workspace_bytes.argtypes = _lib.igated_linear_s8_workspace_bytes.argtypes = [_linearp, C.POINTER(C.c_size_t)]
 _lib.ilinear_s8.argtypes = [_linearp] + [_vp] * 9
 _lib.igated_linear_s8.argtypes = [_linearp] + [_vp] * 11
+_routep, _groupedp, _combinep, _s4p = (C.POINTER(t) for t in (icnn_route_desc, icnn_grouped_desc, icnn_combine_desc, icnn_linear_s4_desc))
+_lib.iroute_top_workspace_bytes.argtypes = [_routep, C.POINTER(C.c_size_t)]
+_lib.iroute_top.argtypes = [_routep] + [_vp] * 8
+_lib.igrouped_linear_s8.argtypes = [_groupedp] + [_vp] * 9
+_lib.igrouped_gated_linear_s8.argtypes = [_groupedp] + [_vp] * 12
+_lib.icombine_rows.argtypes = [_combinep] + [_vp] * 6
+_lib.iweights_s4_bytes.argtypes = [_i32, _i32, C.POINTER(C.c_size_t)]
+_lib.iquantize_weights_s4.argtypes = [C.POINTER(icnn_quantize_s4_desc)] + [_vp] * 4
+_lib.ilinear_s4.argtypes = [_s4p] + [_vp] * 8
+_lib.igated_linear_s4.argtypes = [_s4p] + [_vp] * 10
 _lib.icnn_peak_mfma_i8.argtypes = [_i32, _i32, _vp, _vp]
 _lib.icnn_peak_copy.argtypes = [_vp, _vp, C.c_size_t, _vp]
 
@@ -129,7 +164,8 @@ EXPORTS = ["icnn_version", "icnn_last_error", "icnn_set_tuning", "iconv2d_valida
            "iconv2d_brelu", "iconv2d_brelu_static_ws", "iconv2d_packed_channel_params_bytes", "iconv2d_prepack_channel_params", "iconv2d_brelu_pc",
            "iconv2d_dual_brelu", "iconv2d_dual_brelu_pc", "iconv2d_bottleneck_brelu", "iconv2d_bottleneck_dual_brelu", "iconv2d_pair_brelu", "iconv2d_maxpool_brelu_pc", "iconv2d_bottleneck_brelu_pc", "iconv2d_bottleneck_dual_brelu_pc", "iconv2d_pair_brelu_pc", "iconv2d_triple_brelu", "iconv2d_triple_brelu_pc", "iconv2d_twin_brelu", "iconv2d_twin_last_brelu", "iconv2d_maxpool_brelu", "iconv2d_chain_brelu", "iconv2d_chain_split", "icnn_run_calls", "icnn_lanes_create", "icnn_lanes_destroy", "icnn_run_lanes", "iadd_rescale", "iconcat", "imaxpool2d_u8", "iavgpool_global_u8",
            "irenormalize_u8", "irms_norm_s8", "iquantize_rows_s8", "ilinear_s8_workspace_bytes", "ilinear_s8", "igated_linear_s8_workspace_bytes",
-           "igated_linear_s8", "icnn_peak_mfma_i8", "icnn_peak_copy"]
+           "igated_linear_s8", "iroute_top_workspace_bytes", "iroute_top", "igrouped_linear_s8", "igrouped_gated_linear_s8", "icombine_rows",
+           "iweights_s4_bytes", "iquantize_weights_s4", "ilinear_s4", "igated_linear_s4", "icnn_peak_mfma_i8", "icnn_peak_copy"]
 
 
 def _ptr(t):
@@ -188,7 +224,7 @@ def _strided(d, kw, widths):
     for k, v in kw.items():
         if not hasattr(d, k):
             raise AttributeError(k)
-        setattr(d, k, float(v) if k == "eps" else int(v))
+        setattr(d, k, float(v) if k in ("eps", "scale") else int(v))
     for k, width in widths.items():
         if k not in kw:
             setattr(d, k, getattr(d, width))
@@ -208,6 +244,49 @@ def linear_desc(**kw):
     d = icnn_linear_desc()
     d.dtype = ICNN_BF16
     return _strided(d, kw, {"x_stride": "k", "w_stride": "k", "res_stride": "n", "y_stride": "n"})
+
+
+def route_desc(**kw):
+    """Descriptor of iroute_top: dense rows of float32 logits, a softmax over all experts, gates as they are, where not given otherwise."""
+    d = icnn_route_desc()
+    d.dtype, d.scale = ICNN_F32, 1.0
+    return _strided(d, kw, {"logits_stride": "experts"})
+
+
+def grouped_desc(**kw):
+    """Descriptor of igrouped_linear_s8 and igrouped_gated_linear_s8: dense rows and weights, a row of x for each position, no activation, bfloat16 results, where not
+    given otherwise."""
+    d = icnn_grouped_desc()
+    d.dtype = ICNN_BF16
+    _strided(d, kw, {"x_rows": "rows", "x_stride": "k", "w_stride": "k", "y_stride": "n"})
+    if "expert_stride" not in kw:
+        d.expert_stride = d.n * d.w_stride
+    return d
+
+
+def combine_desc(**kw):
+    """Descriptor of icombine_rows: dense rows, all of bfloat16, where not given otherwise; v has a row for each choice."""
+    d = icnn_combine_desc()
+    d.dtype = ICNN_BF16
+    d.v_dtype = kw.get("dtype", ICNN_BF16)
+    _strided(d, kw, {"v_stride": "c", "res_stride": "c", "y_stride": "c"})
+    if "v_rows" not in kw:
+        d.v_rows = d.rows * d.top
+    return d
+
+
+def linear_s4_desc(**kw):
+    """Descriptor of ilinear_s4 and igated_linear_s4: dense rows, groups of 128 numbers with float16 scales, no activation, bfloat16 results, where not given otherwise."""
+    d = icnn_linear_s4_desc()
+    d.dtype, d.group, d.scale_dtype = ICNN_BF16, 128, ICNN_F16
+    return _strided(d, kw, {"x_stride": "k", "res_stride": "n", "y_stride": "n"})
+
+
+def quantize_s4_desc(**kw):
+    """Descriptor of iquantize_weights_s4: dense rows of float32, groups of 128 numbers with float16 scales, where not given otherwise."""
+    d = icnn_quantize_s4_desc()
+    d.dtype, d.group, d.scale_dtype = ICNN_F32, 128, ICNN_F16
+    return _strided(d, kw, {"w_stride": "k"})
 
 
 def add_desc(**kw):
@@ -383,7 +462,9 @@ def iconv2d_chain_split(descs):
     return list(lens[:k.value])
 
 
-FEED_FORWARD = {"rms_norm": ICNN_CALL_RMS_NORM, "quantize_rows": ICNN_CALL_QUANTIZE_ROWS, "linear": ICNN_CALL_LINEAR, "gated_linear": ICNN_CALL_GATED_LINEAR}
+FEED_FORWARD = {"rms_norm": ICNN_CALL_RMS_NORM, "quantize_rows": ICNN_CALL_QUANTIZE_ROWS, "linear": ICNN_CALL_LINEAR, "gated_linear": ICNN_CALL_GATED_LINEAR,
+                "route": ICNN_CALL_ROUTE, "combine": ICNN_CALL_COMBINE, "grouped_linear": ICNN_CALL_GROUPED_LINEAR,
+                "grouped_gated_linear": ICNN_CALL_GROUPED_GATED_LINEAR, "linear_s4": ICNN_CALL_LINEAR_S4, "gated_linear_s4": ICNN_CALL_GATED_LINEAR_S4}
 
 
 class Calls:
@@ -528,6 +609,51 @@ def igated_linear_s8_workspace_bytes(desc):
 def igated_linear_s8(desc, x, x_scale, w_gate, gate_scale, gate_bias, w_up, up_scale, up_bias, y, workspace=None, stream=None):
     return _check(_lib.igated_linear_s8(C.byref(desc), _ptr(x), _ptr(x_scale), _ptr(w_gate), _ptr(gate_scale), _ptr(gate_bias), _ptr(w_up),
                                         _ptr(up_scale), _ptr(up_bias), _ptr(y), _ptr(workspace), _stream(stream)))
+
+
+def iroute_top_workspace_bytes(desc):
+    size = C.c_size_t()
+    _check(_lib.iroute_top_workspace_bytes(C.byref(desc), C.byref(size)))
+    return size.value
+
+
+def iroute_top(desc, logits, expert, gate, place, token, offsets, workspace=None, stream=None):
+    return _check(_lib.iroute_top(C.byref(desc), _ptr(logits), _ptr(expert), _ptr(gate), _ptr(place), _ptr(token), _ptr(offsets), _ptr(workspace),
+                                  _stream(stream)))
+
+
+def igrouped_linear_s8(desc, x, x_scale, index, offsets, w, w_scale, bias, y, stream=None):
+    return _check(_lib.igrouped_linear_s8(C.byref(desc), _ptr(x), _ptr(x_scale), _ptr(index), _ptr(offsets), _ptr(w), _ptr(w_scale), _ptr(bias), _ptr(y),
+                                          _stream(stream)))
+
+
+def igrouped_gated_linear_s8(desc, x, x_scale, index, offsets, w_gate, gate_scale, gate_bias, w_up, up_scale, up_bias, y, stream=None):
+    return _check(_lib.igrouped_gated_linear_s8(C.byref(desc), _ptr(x), _ptr(x_scale), _ptr(index), _ptr(offsets), _ptr(w_gate), _ptr(gate_scale),
+                                                _ptr(gate_bias), _ptr(w_up), _ptr(up_scale), _ptr(up_bias), _ptr(y), _stream(stream)))
+
+
+def icombine_rows(desc, v, gate, place, residual, y, stream=None):
+    return _check(_lib.icombine_rows(C.byref(desc), _ptr(v), _ptr(gate), _ptr(place), _ptr(residual), _ptr(y), _stream(stream)))
+
+
+def iweights_s4_bytes(n, k):
+    size = C.c_size_t()
+    _check(_lib.iweights_s4_bytes(int(n), int(k), C.byref(size)))
+    return size.value
+
+
+def iquantize_weights_s4(desc, w, w_packed, w_scale, stream=None):
+    return _check(_lib.iquantize_weights_s4(C.byref(desc), _ptr(w), _ptr(w_packed), _ptr(w_scale), _stream(stream)))
+
+
+def ilinear_s4(desc, x, x_scale, w_packed, w_scale, bias, residual, y, stream=None):
+    return _check(_lib.ilinear_s4(C.byref(desc), _ptr(x), _ptr(x_scale), _ptr(w_packed), _ptr(w_scale), _ptr(bias), _ptr(residual), _ptr(y),
+                                  _stream(stream)))
+
+
+def igated_linear_s4(desc, x, x_scale, gate_packed, gate_scale, gate_bias, up_packed, up_scale, up_bias, y, stream=None):
+    return _check(_lib.igated_linear_s4(C.byref(desc), _ptr(x), _ptr(x_scale), _ptr(gate_packed), _ptr(gate_scale), _ptr(gate_bias), _ptr(up_packed),
+                                        _ptr(up_scale), _ptr(up_bias), _ptr(y), _stream(stream)))
 
 
 def icnn_peak_mfma_i8(blocks, iters, sink, stream=None):

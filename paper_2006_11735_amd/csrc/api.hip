@@ -1446,6 +1446,263 @@ int igated_linear_s8(const icnn_linear_desc *desc, const void *x, const float *x
     return run_linear(desc, a, workspace, stream, "igated_linear_s8");
 }
 
+// ---- layers of experts
+
+static int check_route(const icnn_route_desc *d)
+{
+    if (!d) return fail(ICNN_E_NULL, "descriptor is NULL");
+    if (d->experts < 1 || d->experts > kMostExperts) return fail(ICNN_E_SHAPE, "experts %d must be in [1, %d]", d->experts, kMostExperts);
+    if (d->top < 1 || d->top > d->experts || d->top > kMostTop) return fail(ICNN_E_SHAPE, "top %d must be in [1, min(experts, %d)]", d->top, kMostTop);
+    if (d->rows < 0 || d->rows > kMostRows / d->top) return fail(ICNN_E_SHAPE, "rows %lld: rows * top must be in [0, 2^31 - 2^16]", (long long)d->rows);
+    if (!is_stream(d->dtype)) return fail(ICNN_E_PARAM, "dtype %d must be ICNN_F32, ICNN_F16 or ICNN_BF16", d->dtype);
+    if (d->score != ICNN_ROUTE_SOFTMAX && d->score != ICNN_ROUTE_SIGMOID) return fail(ICNN_E_PARAM, "unknown score %d", d->score);
+    if (d->normalise != 0 && d->normalise != 1) return fail(ICNN_E_PARAM, "normalise must be 0 or 1");
+    if (!std::isfinite(d->scale)) return fail(ICNN_E_PARAM, "scale must be finite");
+    return check_stride("logits_stride", d->logits_stride, d->experts, d->rows);
+}
+
+int iroute_top_workspace_bytes(const icnn_route_desc *desc, size_t *bytes)
+{
+    if (int rc = check_route(desc)) return rc;
+    if (!bytes) return fail(ICNN_E_NULL, "bytes is NULL");
+    *bytes = route_workspace(desc->rows, desc->experts);
+    return ICNN_OK;
+}
+
+int iroute_top(const icnn_route_desc *d, const void *logits, int32_t *expert, float *gate, int32_t *place, int32_t *token, int32_t *offsets,
+               void *workspace, void *stream)
+{
+    if (int rc = check_route(d)) return rc;
+    if (!offsets) return fail(ICNN_E_NULL, "offsets must not be NULL");
+    const size_t bytes = route_workspace(d->rows, d->experts);
+    if (d->rows && (!logits || !expert || !gate || !place || !token)) return fail(ICNN_E_NULL, "logits, expert, gate, place and token must not be NULL");
+    if (bytes && !workspace) return fail(ICNN_E_NULL, "%lld rows need a workspace", (long long)d->rows);
+    const int item = item_of(d->dtype);
+    if (!aligned_to(logits, item)) return fail(ICNN_E_ALIGN, "logits must be aligned to their elements");
+    for (const void *p : {(const void *)expert, (const void *)gate, (const void *)place, (const void *)token, (const void *)offsets})
+        if (!aligned_to(p, 4)) return fail(ICNN_E_ALIGN, "expert, gate, place, token and offsets must be 4-byte aligned");
+    if (!aligned_to(workspace, 16)) return fail(ICNN_E_ALIGN, "workspace must be 16-byte aligned");
+    if (d->rows) {
+        const int64_t many = d->rows * d->top;
+        Rows all[7] = {rows_of(expert, 1, many, many, 4), rows_of(gate, 1, many, many, 4), rows_of(place, 1, many, many, 4), rows_of(token, 1, many, many, 4),
+                       rows_of(offsets, 1, d->experts + 1, d->experts + 1, 4), rows_of(logits, d->rows, d->logits_stride, d->experts, item),
+                       rows_of(workspace, 1, (int64_t)bytes, (int64_t)bytes, 1)};
+        const int n = bytes ? 7 : 6;
+        for (int i = 0; i < n; ++i)
+            for (int j = 0; j < i; ++j)
+                if (share(all[i], all[j])) return fail(ICNN_E_UNSUPPORTED, "an output or the workspace overlaps another or the logits");
+    }
+    RouteArgs a;
+    a.logits = logits; a.expert = expert; a.place = place; a.token = token; a.offsets = offsets; a.gate = gate; a.counts = (uint16_t *)workspace;
+    a.rows = d->rows; a.ld = d->logits_stride;
+    a.experts = d->experts; a.top = d->top; a.dtype = d->dtype; a.score = d->score; a.normalise = d->normalise; a.scale = d->scale;
+    return launched(launch_route(a, (hipStream_t)stream), "iroute_top");
+}
+
+int icombine_rows(const icnn_combine_desc *d, const void *v, const float *gate, const int32_t *place, const void *residual, void *y, void *stream)
+{
+    if (!d) return fail(ICNN_E_NULL, "descriptor is NULL");
+    if (d->c < 1 || d->c > (1 << 20)) return fail(ICNN_E_SHAPE, "c %d must be in [1, 2^20]", d->c);
+    if (d->top < 1 || d->top > kMostTop) return fail(ICNN_E_SHAPE, "top %d must be in [1, %d]", d->top, kMostTop);
+    if (d->rows < 0 || d->rows > kMostRows / d->top) return fail(ICNN_E_SHAPE, "rows %lld: rows * top must be in [0, 2^31 - 2^16]", (long long)d->rows);
+    if (d->v_rows < 0 || d->v_rows > kMostRows) return fail(ICNN_E_SHAPE, "v_rows %lld must be in [0, 2^31 - 2^16]", (long long)d->v_rows);
+    if (!is_stream(d->dtype) || !is_stream(d->v_dtype)) return fail(ICNN_E_PARAM, "dtype and v_dtype must be ICNN_F32, ICNN_F16 or ICNN_BF16");
+    if (int rc = check_stride("v_stride", d->v_stride, d->c, d->v_rows)) return rc;
+    if (int rc = check_stride("y_stride", d->y_stride, d->c, d->rows)) return rc;
+    if (residual)
+        if (int rc = check_stride("res_stride", d->res_stride, d->c, d->rows)) return rc;
+    if (d->rows == 0) return ICNN_OK;
+    if ((!v && d->v_rows) || !gate || !place || !y) return fail(ICNN_E_NULL, "v, gate, place and y must not be NULL");
+    const int item = item_of(d->dtype), vitem = item_of(d->v_dtype);
+    if (!aligned_to(v, vitem) || !aligned_to(residual, item) || !aligned_to(y, item) || !aligned_to(gate, 4) || !aligned_to(place, 4))
+        return fail(ICNN_E_ALIGN, "v, gate, place, residual and y must be aligned to their elements");
+    const int64_t many = d->rows * d->top;
+    const Rows ry = rows_of(y, d->rows, d->y_stride, d->c, item), rr = rows_of(residual, d->rows, d->res_stride, d->c, item);
+    if (share(ry, rows_of(gate, 1, many, many, 4)) || share(ry, rows_of(place, 1, many, many, 4)) ||
+        (d->v_rows && share(ry, rows_of(v, d->v_rows, d->v_stride, d->c, vitem))) || (residual && share(ry, rr) && !same(ry, rr)))
+        return fail(ICNN_E_UNSUPPORTED, "y overlaps another operand");
+    CombineArgs a;
+    a.v = v; a.res = residual; a.gate = gate; a.place = place; a.y = y;
+    a.rows = d->rows; a.v_rows = d->v_rows; a.ldv = d->v_stride; a.ldr = d->res_stride; a.ldy = d->y_stride;
+    a.top = d->top; a.c = d->c; a.dtype = d->dtype; a.v_dtype = d->v_dtype;
+    return launched(launch_combine(a, (hipStream_t)stream), "icombine_rows");
+}
+
+static int run_grouped(const icnn_grouped_desc *d, GroupedArgs &g, void *stream, const char *what)
+{
+    if (!d) return fail(ICNN_E_NULL, "descriptor is NULL");
+    LinearArgs &a = g.l;
+    if (d->rows < 0 || d->rows > kMostRows) return fail(ICNN_E_SHAPE, "rows %lld must be in [0, 2^31 - 2^16]", (long long)d->rows);
+    if (d->x_rows < 0 || d->x_rows > kMostRows) return fail(ICNN_E_SHAPE, "x_rows %lld must be in [0, 2^31 - 2^16]", (long long)d->x_rows);
+    if (d->k < 1 || d->n < 1 || d->n > (1 << 22)) return fail(ICNN_E_SHAPE, "k and n must be >= 1, n at most 2^22");
+    if (d->k > 131071) return fail(ICNN_E_SHAPE, "k = %d exceeds 131071: int32 accumulation not provably safe", d->k);
+    if (d->experts < 1 || d->experts > kMostExperts) return fail(ICNN_E_SHAPE, "experts %d must be in [1, %d]", d->experts, kMostExperts);
+    if (!is_stream(d->dtype)) return fail(ICNN_E_PARAM, "dtype %d must be ICNN_F32, ICNN_F16 or ICNN_BF16", d->dtype);
+    if (d->act < ICNN_ACT_NONE || d->act > ICNN_ACT_GELU_TANH) return fail(ICNN_E_PARAM, "unknown act %d", d->act);
+    if (int rc = check_stride("x_stride", d->x_stride, d->k, d->x_rows)) return rc;
+    if (int rc = check_stride("w_stride", d->w_stride, d->k, d->n)) return rc;
+    if (int rc = check_stride("expert_stride", d->expert_stride, (d->n - 1) * d->w_stride + d->k, d->experts)) return rc;
+    if (int rc = check_stride("y_stride", d->y_stride, d->n, d->rows)) return rc;
+    if (!grouped_fits(d->rows, d->experts, d->n))
+        return fail(ICNN_E_SHAPE, "%lld rows of %d experts and n = %d: more outputs than a launch holds", (long long)d->rows, d->experts, d->n);
+    if (!g.index && d->x_rows < d->rows) return fail(ICNN_E_SHAPE, "x_rows %lld: without an index there is one for each of the %lld rows", (long long)d->x_rows, (long long)d->rows);
+    if (d->rows == 0 || d->x_rows == 0) return ICNN_OK;
+    if (!a.x || !a.xs || !a.w || !a.ws || !a.y || !g.offsets) return fail(ICNN_E_NULL, "x, x_scale, offsets, w, w_scale and y must not be NULL");
+    for (const void *p : {(const void *)a.xs, (const void *)a.ws, (const void *)a.ws2, (const void *)a.bias, (const void *)a.bias2, (const void *)g.index, (const void *)g.offsets})
+        if (!aligned_to(p, 4)) return fail(ICNN_E_ALIGN, "scales, biases, index and offsets must be 4-byte aligned");
+    const int item = item_of(d->dtype);
+    if (!aligned_to(a.y, item)) return fail(ICNN_E_ALIGN, "y must be aligned to its elements");
+    const Rows y = rows_of(a.y, d->rows, d->y_stride, d->n, item);
+    const int64_t all = (int64_t)d->experts * d->n, span = (d->experts - 1) * d->expert_stride + (d->n - 1) * d->w_stride + d->k;
+    const Operand in[] = {
+        {"x", a.x, rows_of(a.x, d->x_rows, d->x_stride, d->k, 1)}, {"w", a.w, rows_of(a.w, 1, span, span, 1)}, {"w_up", a.w2, rows_of(a.w2, 1, span, span, 1)},
+        {"x_scale", a.xs, rows_of(a.xs, 1, d->x_rows, d->x_rows, 4)}, {"w_scale", a.ws, rows_of(a.ws, 1, all, all, 4)},
+        {"up_scale", a.ws2, rows_of(a.ws2, 1, all, all, 4)}, {"bias", a.bias, rows_of(a.bias, 1, all, all, 4)}, {"up_bias", a.bias2, rows_of(a.bias2, 1, all, all, 4)},
+        {"index", g.index, rows_of(g.index, 1, d->rows, d->rows, 4)}, {"offsets", g.offsets, rows_of(g.offsets, 1, d->experts + 1, d->experts + 1, 4)}};
+    for (const Operand &o : in)
+        if (o.p && share(y, o.r)) return fail(ICNN_E_UNSUPPORTED, "y overlaps %s", o.name);
+    a.M = (int)d->rows;
+    a.N = d->n;
+    a.K = d->k;
+    a.ldx = d->x_stride;
+    a.ldw = d->w_stride;
+    a.ldy = d->y_stride;
+    a.act = d->act;
+    a.dtype = d->dtype;
+    g.x_rows = d->x_rows;
+    g.expert_stride = d->expert_stride;
+    g.experts = d->experts;
+    return launched(launch_grouped(g, (hipStream_t)stream), what);
+}
+
+int igrouped_linear_s8(const icnn_grouped_desc *desc, const void *x, const float *x_scale, const int32_t *index, const int32_t *offsets, const void *w,
+                       const float *w_scale, const float *bias, void *y, void *stream)
+{
+    GroupedArgs g = {};
+    g.l.x = (const int8_t *)x; g.l.xs = x_scale; g.index = index; g.offsets = offsets;
+    g.l.w = (const int8_t *)w; g.l.ws = w_scale; g.l.bias = bias;
+    g.l.y = y;
+    return run_grouped(desc, g, stream, "igrouped_linear_s8");
+}
+
+int igrouped_gated_linear_s8(const icnn_grouped_desc *desc, const void *x, const float *x_scale, const int32_t *index, const int32_t *offsets, const void *w_gate,
+                             const float *gate_scale, const float *gate_bias, const void *w_up, const float *up_scale, const float *up_bias, void *y, void *stream)
+{
+    if (desc && desc->rows && desc->x_rows && (!w_up || !up_scale)) return fail(ICNN_E_NULL, "w_up and up_scale must not be NULL");
+    GroupedArgs g = {};
+    g.l.x = (const int8_t *)x; g.l.xs = x_scale; g.index = index; g.offsets = offsets;
+    g.l.w = (const int8_t *)w_gate; g.l.ws = gate_scale; g.l.bias = gate_bias;
+    g.l.w2 = (const int8_t *)w_up; g.l.ws2 = up_scale; g.l.bias2 = up_bias;
+    g.l.y = y;
+    return run_grouped(desc, g, stream, "igrouped_gated_linear_s8");
+}
+
+// ---- weights of 4 bits
+
+static int check_s4(int64_t k, int64_t n, int group, int scale_dtype)
+{
+    if (k < 1 || n < 1 || n > (1 << 22)) return fail(ICNN_E_SHAPE, "k and n must be >= 1, n at most 2^22");
+    if (k > 131071) return fail(ICNN_E_SHAPE, "k = %lld exceeds 131071", (long long)k);
+    if (group != 32 && group != 64 && group != 128 && group != 256) return fail(ICNN_E_PARAM, "group %d must be 32, 64, 128 or 256", group);
+    if (!is_stream(scale_dtype)) return fail(ICNN_E_PARAM, "scale_dtype %d must be ICNN_F32, ICNN_F16 or ICNN_BF16", scale_dtype);
+    return ICNN_OK;
+}
+
+int iweights_s4_bytes(int32_t n, int32_t k, size_t *bytes)
+{
+    if (int rc = check_s4(k, n, 32, ICNN_F32)) return rc;
+    if (!bytes) return fail(ICNN_E_NULL, "bytes is NULL");
+    *bytes = (size_t)n * (size_t)((k + 31) / 32) * 16;
+    return ICNN_OK;
+}
+
+int iquantize_weights_s4(const icnn_quantize_s4_desc *d, const void *w, void *w_packed, void *w_scale, void *stream)
+{
+    if (!d) return fail(ICNN_E_NULL, "descriptor is NULL");
+    if (int rc = check_s4(d->k, d->n, d->group, d->scale_dtype)) return rc;
+    if (!is_stream(d->dtype)) return fail(ICNN_E_PARAM, "dtype %d must be ICNN_F32, ICNN_F16 or ICNN_BF16", d->dtype);
+    if (int rc = check_stride("w_stride", d->w_stride, d->k, d->n)) return rc;
+    const int64_t groups = (d->k + d->group - 1) / d->group, blocks = (d->k + 31) / 32;
+    if (d->n * groups * (d->group / 32) > ((int64_t)1 << 31)) return fail(ICNN_E_SHAPE, "%d rows of %d numbers: more than a launch holds", d->n, d->k);
+    if (!w || !w_packed || !w_scale) return fail(ICNN_E_NULL, "w, w_packed and w_scale must not be NULL");
+    const int item = item_of(d->dtype), sitem = item_of(d->scale_dtype);
+    if (!aligned_to(w, item) || !aligned_to(w_scale, sitem)) return fail(ICNN_E_ALIGN, "w and w_scale must be aligned to their elements");
+    if (!aligned16(w_packed)) return fail(ICNN_E_ALIGN, "w_packed must be 16-byte aligned");
+    const Rows rw = rows_of(w, d->n, d->w_stride, d->k, item), rp = rows_of(w_packed, 1, d->n * blocks * 16, d->n * blocks * 16, 1),
+               rs = rows_of(w_scale, 1, d->n * groups, d->n * groups, sitem);
+    if (share(rp, rw) || share(rs, rw) || share(rp, rs)) return fail(ICNN_E_UNSUPPORTED, "an output overlaps the input or the other output");
+    QuantizeS4Args a;
+    a.w = w; a.packed = (uint8_t *)w_packed; a.scale = w_scale;
+    a.ld = d->w_stride; a.n = d->n; a.k = d->k; a.group = d->group; a.dtype = d->dtype; a.scale_dtype = d->scale_dtype;
+    return launched(launch_quantize_s4(a, (hipStream_t)stream), "iquantize_weights_s4");
+}
+
+static int run_linear_s4(const icnn_linear_s4_desc *d, LinearS4Args &a, bool gated, void *stream, const char *what)
+{
+    if (!d) return fail(ICNN_E_NULL, "descriptor is NULL");
+    if (d->rows < 0 || d->rows > kMostRows) return fail(ICNN_E_SHAPE, "rows %lld must be in [0, 2^31 - 2^16]", (long long)d->rows);
+    if (int rc = check_s4(d->k, d->n, d->group, d->scale_dtype)) return rc;
+    if (!is_stream(d->dtype)) return fail(ICNN_E_PARAM, "dtype %d must be ICNN_F32, ICNN_F16 or ICNN_BF16", d->dtype);
+    if (d->act < ICNN_ACT_NONE || d->act > ICNN_ACT_GELU_TANH) return fail(ICNN_E_PARAM, "unknown act %d", d->act);
+    if (int rc = check_stride("x_stride", d->x_stride, d->k, d->rows)) return rc;
+    if (int rc = check_stride("y_stride", d->y_stride, d->n, d->rows)) return rc;
+    if (a.res)
+        if (int rc = check_stride("res_stride", d->res_stride, d->n, d->rows)) return rc;
+    if (!s4_fits(d->rows, d->n)) return fail(ICNN_E_SHAPE, "%lld rows and n = %d: more outputs than a launch holds", (long long)d->rows, d->n);
+    if (d->rows == 0) return ICNN_OK;
+    if (!a.x || !a.xs || !a.w || !a.ws || !a.y) return fail(ICNN_E_NULL, "x, x_scale, w, w_scale and y must not be NULL");
+    if (gated && (!a.w2 || !a.ws2)) return fail(ICNN_E_NULL, "w_up and up_scale must not be NULL");
+    const int item = item_of(d->dtype), sitem = item_of(d->scale_dtype);
+    for (const void *p : {(const void *)a.xs, (const void *)a.bias, (const void *)a.bias2})
+        if (!aligned_to(p, 4)) return fail(ICNN_E_ALIGN, "x_scale and biases must be 4-byte aligned");
+    if (!aligned_to(a.ws, sitem) || !aligned_to(a.ws2, sitem)) return fail(ICNN_E_ALIGN, "the weights' scales must be aligned to their elements");
+    if (!aligned16(a.w) || !aligned16(a.w2)) return fail(ICNN_E_ALIGN, "packed weights must be 16-byte aligned");
+    if (!aligned_to(a.y, item) || !aligned_to(a.res, item)) return fail(ICNN_E_ALIGN, "y and residual must be aligned to their elements");
+    a.M = (int)d->rows;
+    a.N = d->n;
+    a.K = d->k;
+    a.ldx = d->x_stride;
+    a.ldr = d->res_stride;
+    a.ldy = d->y_stride;
+    a.ldw = (d->k + 31) / 32 * 16;
+    a.group = d->group;
+    a.groups = (d->k + d->group - 1) / d->group;
+    a.act = d->act;
+    a.dtype = d->dtype;
+    a.scale_dtype = d->scale_dtype;
+    const Rows y = rows_of(a.y, d->rows, d->y_stride, d->n, item);
+    const int64_t packed = d->n * a.ldw, scales = (int64_t)d->n * a.groups;
+    const Operand in[] = {
+        {"x", a.x, rows_of(a.x, d->rows, d->x_stride, d->k, 1)}, {"w", a.w, rows_of(a.w, 1, packed, packed, 1)}, {"w_up", a.w2, rows_of(a.w2, 1, packed, packed, 1)},
+        {"x_scale", a.xs, rows_of(a.xs, 1, d->rows, d->rows, 4)}, {"w_scale", a.ws, rows_of(a.ws, 1, scales, scales, sitem)},
+        {"up_scale", a.ws2, rows_of(a.ws2, 1, scales, scales, sitem)}, {"bias", a.bias, rows_of(a.bias, 1, d->n, d->n, 4)},
+        {"up_bias", a.bias2, rows_of(a.bias2, 1, d->n, d->n, 4)}, {"residual", a.res, rows_of(a.res, d->rows, d->res_stride, d->n, item)}};
+    for (const Operand &o : in)
+        if (o.p && share(y, o.r) && !(o.p == a.res && same(y, o.r))) return fail(ICNN_E_UNSUPPORTED, "y overlaps %s", o.name);
+    return launched(launch_linear_s4(a, (hipStream_t)stream), what);
+}
+
+int ilinear_s4(const icnn_linear_s4_desc *desc, const void *x, const float *x_scale, const void *w_packed, const void *w_scale, const float *bias,
+               const void *residual, void *y, void *stream)
+{
+    LinearS4Args a = {};
+    a.x = (const int8_t *)x; a.xs = x_scale;
+    a.w = (const uint8_t *)w_packed; a.ws = w_scale; a.bias = bias;
+    a.res = residual; a.y = y;
+    return run_linear_s4(desc, a, false, stream, "ilinear_s4");
+}
+
+int igated_linear_s4(const icnn_linear_s4_desc *desc, const void *x, const float *x_scale, const void *gate_packed, const void *gate_scale, const float *gate_bias,
+                     const void *up_packed, const void *up_scale, const float *up_bias, void *y, void *stream)
+{
+    LinearS4Args a = {};
+    a.x = (const int8_t *)x; a.xs = x_scale;
+    a.w = (const uint8_t *)gate_packed; a.ws = gate_scale; a.bias = gate_bias;
+    a.w2 = (const uint8_t *)up_packed; a.ws2 = up_scale; a.bias2 = up_bias;
+    a.y = y;
+    return run_linear_s4(desc, a, true, stream, "igated_linear_s4");
+}
+
 static int run_call(int32_t k, const icnn_call &c, void *stream)
 {
     const void *const *p = c.p;
@@ -1483,6 +1740,20 @@ static int run_call(int32_t k, const icnn_call &c, void *stream)
         break;
     case ICNN_CALL_GATED_LINEAR:
         rc = igated_linear_s8((const icnn_linear_desc *)c.list[0], p[0], f(1), p[2], f(3), f(4), p[5], f(6), f(7), o(8), o(9), stream);
+        break;
+    case ICNN_CALL_ROUTE:
+        rc = iroute_top((const icnn_route_desc *)c.list[0], p[0], (int32_t *)o(1), f(2), (int32_t *)o(3), (int32_t *)o(4), (int32_t *)o(5), o(6), stream);
+        break;
+    case ICNN_CALL_COMBINE: rc = icombine_rows((const icnn_combine_desc *)c.list[0], p[0], f(1), b(2), p[3], o(4), stream); break;
+    case ICNN_CALL_GROUPED_LINEAR:
+        rc = igrouped_linear_s8((const icnn_grouped_desc *)c.list[0], p[0], f(1), b(2), b(3), p[4], f(5), f(6), o(7), stream);
+        break;
+    case ICNN_CALL_GROUPED_GATED_LINEAR:
+        rc = igrouped_gated_linear_s8((const icnn_grouped_desc *)c.list[0], p[0], f(1), b(2), b(3), p[4], f(5), f(6), p[7], f(8), f(9), o(10), stream);
+        break;
+    case ICNN_CALL_LINEAR_S4: rc = ilinear_s4((const icnn_linear_s4_desc *)c.list[0], p[0], f(1), p[2], p[3], f(4), p[5], o(6), stream); break;
+    case ICNN_CALL_GATED_LINEAR_S4:
+        rc = igated_linear_s4((const icnn_linear_s4_desc *)c.list[0], p[0], f(1), p[2], p[3], f(4), p[5], p[6], f(7), o(8), stream);
         break;
     case ICNN_CALL_CONV_MAXPOOL_PC: rc = iconv2d_maxpool_brelu_pc(d[0], i[0], i[1], i[2], p[0], p[1], b(2), p[3], o(4), stream); break;
     case ICNN_CALL_BOTTLENECK_PC:

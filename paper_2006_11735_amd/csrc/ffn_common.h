@@ -25,6 +25,43 @@ hipError_t launch_tokens_linear(const LinearArgs &a, hipStream_t st);
 hipError_t launch_few_linear(const LinearArgs &a, hipStream_t st);
 hipError_t launch_tiled_linear(const LinearArgs &a, const TilePlan &plan, hipStream_t st);
 
+// The router's choice and the sum of the experts' rows (see ffn_route.hip)
+struct RouteArgs {
+    const void *logits;
+    int32_t *expert, *place, *token, *offsets;
+    float *gate;
+    uint16_t *counts;               // [chunks][experts] of a workspace; null where one chunk has all rows
+    long long rows, ld;
+    int experts, top, dtype, score, normalise;
+    float scale;
+};
+
+struct CombineArgs {
+    const void *v, *res;
+    const float *gate;
+    const int32_t *place;
+    void *y;
+    long long rows, v_rows, ldv, ldr, ldy;
+    int top, c, dtype, v_dtype;
+};
+
+// Weights to 4 bits (see ffn_s4.hip)
+struct QuantizeS4Args {
+    const void *w;
+    uint8_t *packed;
+    void *scale;
+    long long ld;
+    int n, k, group, dtype, scale_dtype;
+};
+
+constexpr int kMostExperts = 1024, kMostTop = 16;
+size_t route_workspace(long long rows, int experts);
+hipError_t launch_route(const RouteArgs &a, hipStream_t st);
+hipError_t launch_combine(const CombineArgs &a, hipStream_t st);
+hipError_t launch_grouped(const GroupedArgs &a, hipStream_t st);
+hipError_t launch_linear_s4(const LinearS4Args &a, hipStream_t st);
+hipError_t launch_quantize_s4(const QuantizeS4Args &a, hipStream_t st);
+
 inline LinearTuning linear_tuning() { return {g_tuning.ff_kernel, g_tuning.ff_split}; }
 
 typedef int v4i_any __attribute__((ext_vector_type(4), aligned(1)));       // (global memory takes 16 bytes at any address)

@@ -209,4 +209,38 @@ inline size_t linear_workspace(const LinearArgs &a, const LinearTuning &tuning)
     return most;
 }
 
+// Products whose rows lie in the order of their experts (see ffn_grouped.hip): `l` has the first expert's weights, scales and biases, M is the number of positions
+struct GroupedArgs {
+    LinearArgs l;
+    const int32_t *index;          // x's row of a position; null: the position itself
+    const int32_t *offsets;        // expert e's positions: offsets[e] .. offsets[e + 1] - 1
+    long long x_rows, expert_stride;
+    int experts;
+};
+
+// Groups of `rows` positions of one expert each: as many as there can be, whatever the experts' shares are
+inline long long grouped_slots(long long positions, int experts, int rows)
+{
+    return positions / rows + (positions < experts ? positions : experts);
+}
+
+// What one launch holds by any kernel: 16 x 16 outputs a wave
+constexpr long long kMostTiles = 1 << 25;
+inline bool grouped_fits(long long positions, int experts, int n) { return grouped_slots(positions, experts, 16) <= kMostTiles / ((n + 15ll) / 16); }
+inline bool s4_fits(long long rows, int n) { return (rows + 15) / 16 <= kMostTiles / ((n + 15ll) / 16); }
+
+// A product of 8-bit rows and 4-bit weights, or the two of a gated layer (see ffn_s4.hip)
+struct LinearS4Args {
+    const int8_t *x;
+    const uint8_t *w, *w2;         // rows of `ldw` bytes, blocks of 32 numbers in 16; w2 null: one product
+    const float *xs, *bias, *bias2;
+    const void *ws, *ws2;          // a scale for each group of a row's numbers: [n][groups]
+    const void *res;
+    void *y;
+    long long ldx, ldr, ldy, ldw;
+    int M, N, K;
+    int group, groups;             // numbers of a group (32, 64, 128 or 256), groups of a row
+    int act, dtype, scale_dtype;
+};
+
 }  // namespace icnn

@@ -1,0 +1,204 @@
+"""igrouped_linear_s8 and igrouped_gated_linear_s8 on the GPU against their definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from ff_util import ACTS, DTYPES, Placed, gated64, linear64, to_numpy
+from paper_2006_11735_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def vector(v, offset, dtype=torch.float32):
+    return None if v is None else Placed(1, v.size, dtype, None, offset, torch.from_numpy(np.ascontiguousarray(v)).reshape(1, -1))
+
+
+def run(counts, k, n, dtype="bf16", act="none", *, gated=False, bias=True, index=None, x_rows=None, first=0, behind=0, pads=(0, 0, 0), between=0, offset=0, seed=0,
+        stream=None):
+    """counts: positions of each expert; first, behind: positions in front of them and behind; index: None, or x's row of every position; pads: of the rows of x, w and y;
+    between: elements between two experts' weights; offset: elements in front of every tensor"""
+    g = np.random.default_rng(seed)
+    experts, rows = len(counts), first + sum(counts) + behind
+    torch_dtype, code = DTYPES[dtype]
+    x_rows = x_rows or rows
+    xv = np.clip(np.rint(g.normal(size=(x_rows, k)) * 40), -127, 127).astype(np.int8)
+    xs = g.uniform(0.5, 1.5, size=x_rows).astype(np.float32) / 40
+    bounds = first + np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    layers = [(g.integers(-127, 128, size=(experts, n, k)).astype(np.int8), g.uniform(0.5, 1.5, size=(experts, n)).astype(np.float32) / (70 * k ** 0.5),
+               g.normal(size=(experts, n)).astype(np.float32) if bias else None) for _ in range(2 if gated else 1)]
+    X, XS = Placed(x_rows, k, torch.int8, k + pads[0], offset, torch.from_numpy(xv)), vector(xs, offset)
+    ldw = k + pads[1]
+    step = n * ldw + between
+    W, S, BI = [], [], []
+    for w, s, b in layers:
+        raw = Placed(1, experts * step + 16, torch.int8, None, offset)
+        raw.view.as_strided((experts, n, k), (step, ldw, 1), raw.view.storage_offset()).copy_(torch.from_numpy(w))
+        W.append(raw), S.append(vector(s, offset)), BI.append(vector(b, offset))
+    Y = Placed(rows, n, torch_dtype, n + pads[2], offset)
+    O, I = vector(bounds, offset, torch.int32), None if index is None else vector(index.astype(np.int32), offset, torch.int32)
+    tensors = [t for t in [X, XS, Y, O, I, *W, *S, *BI] if t is not None]
+    for t in tensors:
+        t.snapshot()
+    d = B.grouped_desc(rows=rows, x_rows=x_rows, k=k, n=n, experts=experts, act=ACTS.index(act), dtype=code, x_stride=X.stride, w_stride=ldw, expert_stride=step,
+                       y_stride=Y.stride)
+    before = Y.view.clone()
+    torch.cuda.synchronize()
+    if gated:
+        B.igrouped_gated_linear_s8(d, X, XS, I, O, W[0], S[0], BI[0], W[1], S[1], BI[1], Y, stream=stream)
+    else:
+        B.igrouped_linear_s8(d, X, XS, I, O, W[0], S[0], BI[0], Y, stream=stream)
+    torch.cuda.synchronize()
+    assert all(t.rest_untouched() for t in tensors) and all((t.raw == t.before).all() for t in tensors if t is not Y)
+    got, at = to_numpy(Y.view), np.arange(rows) if index is None else index
+    named = np.zeros(rows, bool)
+    for e in range(experts):
+        rows_of = np.arange(bounds[e], bounds[e + 1])
+        rows_of = rows_of[(at[rows_of] >= 0) & (at[rows_of] < x_rows)]
+        if not len(rows_of):
+            continue
+        named[rows_of] = True
+        xe, xse = xv[at[rows_of]], xs[at[rows_of]]
+        part = [(w[e], s[e], None if b is None else b[e]) for w, s, b in layers]
+        want, tol = gated64(xe, xse, *part[0], *part[1], act, dtype) if gated else linear64(xe, xse, *part[0], act, None, dtype)
+        off = np.abs(got[rows_of] - want) - tol
+        assert (off <= 0).all(), (e, float(off.max()), np.unravel_index(np.argmax(off), off.shape))
+    rest = torch.from_numpy(~named).cuda()
+    assert torch.equal(Y.view[rest].view(torch.uint8), before[rest].view(torch.uint8))
+    return Y.view.clone()
+
+
+SHARES = {"one": [1], "single": [0, 0, 1, 0], "two": [1, 0, 1], "few": [3, 1, 0, 7, 2], "even": [16, 16, 16, 16], "odd": [17, 0, 33, 1, 64, 65, 15],
+          "popular": [0, 200, 3, 0, 0, 9], "large": [129, 257, 0, 300, 128], "many": [2, 0, 5, 1] * 40}
+
+
+@pytest.mark.parametrize("share", list(SHARES))
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("k,n", [(256, 192), (129, 65)])
+def test_shares(share, gated, k, n):
+    counts = SHARES[share]
+    g = np.random.default_rng(len(share))
+    run(counts, k, n, "f32", "silu" if gated else "none", gated=gated, seed=1)
+    x_rows = max(1, sum(counts) // 2)
+    run(counts, k, n, "f32", "silu" if gated else "none", gated=gated, index=g.integers(0, x_rows, size=sum(counts)), x_rows=x_rows, seed=2)
+
+
+@pytest.mark.parametrize("k", [1, 2, 15, 16, 17, 48, 63, 64, 65, 127, 128, 130, 255, 256, 511, 1001, 2048, 5000])
+@pytest.mark.parametrize("counts,n", [([1, 1], 33), ([20, 3, 40], 70), ([130, 7, 200], 140)])
+def test_depths(k, counts, n):
+    run(counts, k, n, "f32", seed=k)
+    run(counts, k, n, "f32", "silu", gated=True, seed=k)
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 8, 15, 16, 17, 31, 33, 64, 127, 128, 129, 255, 257, 1000])
+@pytest.mark.parametrize("counts,k", [([1, 0, 1], 512), ([20, 9], 256), ([90, 130], 256)])
+def test_widths(n, counts, k):
+    run(counts, k, n, "f16", seed=n)
+    run(counts, k, n, "f16", "gelu_tanh", gated=True, seed=n)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("counts", [[1, 1], [10, 37], [200, 140]])
+def test_types_and_activations(dtype, act, counts):
+    run(counts, 384, 272, dtype, act, seed=1)
+    run(counts, 384, 272, dtype, act, bias=False, gated=True, seed=4)
+
+
+@pytest.mark.parametrize("pads,between,offset", [((16, 32, 8), 64, 0), ((16, 16, 16), 0, 16), ((0, 0, 0), 0, 1), ((1, 3, 5), 7, 5), ((16, 0, 0), 1, 0), ((0, 16, 1), 16, 0),
+                                                 ((8, 8, 8), 8, 8), ((4, 4, 4), 4, 4)])
+@pytest.mark.parametrize("counts,k,n", [([1, 1], 320, 144), ([20, 9], 320, 144), ([140, 40], 640, 272), ([140, 40], 333, 111)])
+def test_strides_and_offsets(pads, between, offset, counts, k, n):
+    g = np.random.default_rng(3)
+    index = g.permutation(sum(counts))
+    run(counts, k, n, "f16", "gelu", pads=pads, between=between, offset=offset, seed=7, index=index)
+    run(counts, k, n, "bf16", "silu", gated=True, pads=pads, between=between, offset=offset, seed=8)
+
+
+@pytest.mark.parametrize("counts", [[1, 0], [6, 30], [150, 3, 200]])
+@pytest.mark.parametrize("gated", [False, True])
+def test_positions_of_no_expert_and_rows_that_there_are_not(counts, gated):
+    g = np.random.default_rng(4)
+    run(counts, 256, 160, "bf16", gated=gated, first=5, behind=70, seed=5)
+    rows = sum(counts) + 40
+    index = g.integers(-4, 60, size=rows)              # of 50 rows
+    index[0], index[-1] = np.iinfo(np.int32).min, np.iinfo(np.int32).max
+    run(counts, 256, 160, "bf16", gated=gated, behind=40, index=index, x_rows=50, seed=6)
+
+
+@pytest.mark.parametrize("counts,k,n,gated", [([1, 1], 16384, 512, False), ([4, 3, 9], 8192, 1024, True), ([0] * 30 + [64], 12288, 128, False), ([300, 100], 8192, 256, True),
+                                              ([512, 200, 77], 1024, 2048, False), ([777, 0, 400], 512, 1111, True), ([1024, 1500], 2048, 512, False)])
+def test_larger_products(counts, k, n, gated):
+    run(counts, k, n, "bf16", "silu" if gated else "none", gated=gated, seed=5)
+
+
+@pytest.mark.parametrize("offsets", [[0, 5, 3, 40], [-7, 10, 20, 99], [50, 40, 30, 20], [2 ** 31 - 1, -2 ** 31, 0, 40], [40, 40, 40, 40], [0, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1]])
+@pytest.mark.parametrize("rows", [40, 3])
+def test_offsets_that_are_none_write_no_other_memory(offsets, rows):
+    k, n = 128, 48
+    X, Y = Placed(rows, k, torch.int8, values=torch.ones((rows, k))), Placed(rows, n, torch.float32)
+    one = torch.ones(256, device="cuda:0")
+    w = torch.ones((3, n, k), dtype=torch.int8, device="cuda:0")
+    Y.snapshot()
+    before = Y.view.clone()
+    B.igrouped_linear_s8(B.grouped_desc(rows=rows, k=k, n=n, experts=3, dtype=B.ICNN_F32), X, one, None, torch.tensor(offsets, device="cuda:0").to(torch.int32), w, one, None, Y)
+    torch.cuda.synchronize()
+    assert Y.rest_untouched()
+    same = (Y.view.view(torch.int32) == before.view(torch.int32)).all(1)
+    assert (same | (Y.view == k).all(1)).all()
+
+
+def test_experts_of_equal_weights_agree_with_the_dense_product():
+    """Sums are exact, so a row's result depends on nothing else: grouped and dense kernels give the same bits."""
+    g = torch.Generator(device="cuda:0").manual_seed(1)
+    rows, k, n = 500, 1024, 768
+    x = torch.randint(-127, 128, (rows, k), generator=g, device="cuda:0", dtype=torch.int8)
+    xs, ws, bias = torch.rand(rows, generator=g, device="cuda:0"), torch.rand(n, generator=g, device="cuda:0") / k, torch.randn(n, generator=g, device="cuda:0")
+    w = torch.randint(-127, 128, (n, k), generator=g, device="cuda:0", dtype=torch.int8)
+    want, got = (torch.zeros((rows, n), dtype=torch.bfloat16, device="cuda:0") for _ in range(2))
+    B.ilinear_s8(B.linear_desc(rows=rows, k=k, n=n, act=B.ICNN_ACT_SILU), x, xs, w, ws, bias, None, want)
+    for bounds in ([0, 1, 2, 3, 500], [0, 0, 250, 250, 500], [0, 100, 220, 390, 500]):
+        B.igrouped_linear_s8(B.grouped_desc(rows=rows, k=k, n=n, experts=4, act=B.ICNN_ACT_SILU), x, xs, None, torch.tensor(bounds, dtype=torch.int32, device="cuda:0"),
+                             w.repeat(4, 1, 1), ws.repeat(4), bias.repeat(4), got.zero_())
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), bounds
+
+
+def test_nothing_to_do():
+    d = B.grouped_desc(rows=0, k=64, n=32, experts=4)
+    B.igrouped_linear_s8(d, *[None] * 8)
+    B.igrouped_gated_linear_s8(d, *[None] * 11)
+    run([0, 0, 0], 64, 32, behind=9)
+
+
+@pytest.mark.parametrize("rows", [3, 70, 300])
+def test_rows_and_experts_beyond_32_bits(rows):
+    """The last rows of x and y, and the last expert's weights, lie more than 2^32 bytes behind the first."""
+    k, n, experts = 256, 128, 3
+    stride, step = ((1 << 32) // (rows - 1) + 4096) // 4096 * 4096, (1 << 31) + 4096
+    g = np.random.default_rng(3)
+    x = torch.empty((rows - 1) * stride + k, dtype=torch.int8, device="cuda:0")
+    y = torch.empty((rows - 1) * stride + n, dtype=torch.float16, device="cuda:0")
+    w = torch.empty((experts - 1) * step + n * k, dtype=torch.int8, device="cuda:0")
+    xv, wv = g.integers(-127, 128, size=(rows, k)).astype(np.int8), g.integers(-127, 128, size=(experts, n, k)).astype(np.int8)
+    xs, ws = g.uniform(0.5, 1.5, size=rows).astype(np.float32) / 40, g.uniform(0.5, 1.5, size=(experts, n)).astype(np.float32) / 1000
+    x.as_strided((rows, k), (stride, 1)).copy_(torch.from_numpy(xv))
+    w.as_strided((experts, n, k), (step, k, 1)).copy_(torch.from_numpy(wv))
+    bounds = [0, rows // 3, rows // 2, rows]
+    index = g.permutation(rows).astype(np.int32)
+    dev = lambda v: torch.from_numpy(np.ascontiguousarray(v)).to("cuda:0")  # noqa: E731
+    d = B.grouped_desc(rows=rows, k=k, n=n, experts=experts, x_stride=stride, y_stride=stride, expert_stride=step, dtype=B.ICNN_F16)
+    XS, WS, O = dev(xs), dev(ws), torch.tensor(bounds, dtype=torch.int32, device="cuda:0")
+    for idx in (None, index):
+        B.igrouped_linear_s8(d, x, XS, None if idx is None else dev(idx), O, w, WS, None, y)
+        torch.cuda.synchronize()
+        at = np.arange(rows) if idx is None else idx
+        got = to_numpy(y.as_strided((rows, n), (stride, 1)))
+        for e in range(experts):
+            r = np.arange(bounds[e], bounds[e + 1])
+            want, tol = linear64(xv[at[r]], xs[at[r]], wv[e], ws[e], None, "none", None, "f16")
+            assert (np.abs(got[r] - want) <= tol).all()
+
+
+@pytest.mark.parametrize("counts", [[1, 1], [9, 20], [300, 80]])
+def test_on_another_stream(counts):
+    run(counts, 512, 256, gated=True, stream=torch.cuda.Stream())
