@@ -59,6 +59,7 @@ size_t route_workspace(long long rows, int experts);
 hipError_t launch_route(const RouteArgs &a, hipStream_t st);
 hipError_t launch_combine(const CombineArgs &a, hipStream_t st);
 hipError_t launch_grouped(const GroupedArgs &a, hipStream_t st);
+hipError_t launch_grouped_tiled(const GroupedArgs &a, int tile, hipStream_t st);
 hipError_t launch_linear_s4(const LinearS4Args &a, hipStream_t st);
 hipError_t launch_quantize_s4(const QuantizeS4Args &a, hipStream_t st);
 

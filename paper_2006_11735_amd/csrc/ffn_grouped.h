@@ -9,6 +9,20 @@ struct Place {
     int expert, m0, end;
 };
 
+// Groups of ROWS positions that there are
+template <int ROWS>
+__device__ __forceinline__ int groups_of(const GroupedArgs &g)
+{
+    int all = 0;
+    for (int e = threadIdx.x & 63; e < g.experts; e += 64) {
+        const int lo = min(max(g.offsets[e], 0), g.l.M), hi = min(max(g.offsets[e + 1], lo), g.l.M);
+        all += (hi - lo + ROWS - 1) / ROWS;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
+    return __builtin_amdgcn_readfirstlane(all);
+}
+
 // The `slot`-th group of ROWS positions (the last one of an expert may have fewer), expert by expert.  A wave asks, all of its lanes together; the answer is the same in
 // all.  Whatever the offsets hold, the positions returned are in [0, M).
 template <int ROWS>
@@ -49,11 +63,12 @@ __device__ __forceinline__ int row_of(const GroupedArgs &g, int m)
     return r >= 0 && r < g.x_rows ? r : -1;
 }
 
-// The operands of expert e's product
+// The operands of expert e's product, whose positions end at `end`
 template <bool GATED>
-__device__ __forceinline__ LinearArgs of_expert(const GroupedArgs &g, int e)
+__device__ __forceinline__ LinearArgs of_expert(const GroupedArgs &g, int e, int end)
 {
     LinearArgs a = g.l;
+    a.M = end;
     const long long first = (long long)e * a.N;
     a.w += e * g.expert_stride;
     a.ws += first;

@@ -224,6 +224,54 @@ inline long long grouped_slots(long long positions, int experts, int rows)
     return positions / rows + (positions < experts ? positions : experts);
 }
 
+// Operands' offsets in a tile within 2 GiB: rows of an index lie anywhere in x
+inline bool grouped_rows_near(const GroupedArgs &a) { return a.index ? a.l.ldx <= (0x7ff00000ll / (a.x_rows > 0 ? a.x_rows : 1)) : a.l.ldx <= (1 << 22); }
+inline bool grouped_tiled_takes(const GroupedArgs &a) { return a.l.K >= 16 && a.l.ldw <= (1 << 22) && grouped_rows_near(a); }
+inline bool grouped_few_takes(const GroupedArgs &a) { return a.l.K >= 16 && a.l.ldw <= (1 << 26); }
+inline bool grouped_tokens_takes(const GroupedArgs &a) { return a.l.K >= 16 && a.l.K <= 32768 && a.l.M <= 64; }
+
+struct GroupedPlan {
+    LinearKernel kernel;
+    int tile;                      // of LinearKernel::tiled: its place in kTiles
+    int rows;                      // of LinearKernel::few: positions a group, 16, 32 or 64
+};
+
+// The experts' shares are not known here: they are taken to be even over those that so many positions are expected to reach, E (1 - exp(-M / E)).
+inline GroupedPlan plan_grouped(const GroupedArgs &a, const LinearTuning &tuning, float step)
+{
+    const int force = tuning.kernel;
+    const float positions = (float)a.l.M, experts = (float)a.experts, reached = experts * (1.f - __builtin_expf(-positions / experts)), share = positions / reached;
+    GroupedPlan p = {LinearKernel::plain, 0, 16};
+    // (token by token an expert's weights are read for each of its positions)
+    if (grouped_tokens_takes(a) && (force == 2 || (force == 0 && share <= 1.3f))) {
+        p.kernel = LinearKernel::tokens;
+        return p;
+    }
+    const bool few = grouped_few_takes(a), tiled = grouped_tiled_takes(a);
+    if (few && (force == 3 || (force == 0 && (!tiled || share <= 24.f)))) {
+        p.kernel = LinearKernel::few;
+        p.rows = share <= 16.f ? 16 : share <= 32.f ? 32 : 64;
+        return p;
+    }
+    if (!tiled || (force != 0 && force < 4)) return p;
+    p.kernel = LinearKernel::tiled;
+    float best = 0.f;
+    const float steps = (float)((a.l.K + 127) / 128);
+    for (int c = 0; c < kTileKinds; ++c) {
+        const TileCost &t = kTiles[c];
+        if (force >= 4 && c != force - 4) continue;
+        const float tiles = reached * __builtin_ceilf(share / (float)t.m) * (float)(((a.l.w2 ? 2ll : 1ll) * a.l.N + t.n - 1) / t.n);
+        const float turns = __builtin_ceilf(tiles / (float)t.held), on = tiles < (float)t.held ? tiles / 256.f : (float)t.held / 256.f;
+        const float full = t.held == 256 ? on : on < 1.f ? 0.25f * on : 0.25f + 0.75f * (on - 1.f);
+        const float us = turns * (t.fixed + steps * step * (t.few + (t.all - t.few) * full));
+        if (best == 0.f || us < best) {
+            best = us;
+            p.tile = c;
+        }
+    }
+    return p;
+}
+
 // What one launch holds by any kernel: 16 x 16 outputs a wave
 constexpr long long kMostTiles = 1 << 25;
 inline bool grouped_fits(long long positions, int experts, int n) { return grouped_slots(positions, experts, 16) <= kMostTiles / ((n + 15ll) / 16); }

@@ -202,3 +202,28 @@ def test_rows_and_experts_beyond_32_bits(rows):
 @pytest.mark.parametrize("counts", [[1, 1], [9, 20], [300, 80]])
 def test_on_another_stream(counts):
     run(counts, 512, 256, gated=True, stream=torch.cuda.Stream())
+
+
+@pytest.fixture
+def kernel():
+    yield lambda k: B.icnn_set_tuning("ff_kernel", k)
+    B.icnn_set_tuning("reset")
+
+
+@pytest.mark.parametrize("which,counts", [(1, [3, 0, 40]), (2, [1, 0, 2, 5]), (2, [20, 3, 0, 17]), (3, [1, 0, 30]), (3, [64, 0, 65, 17])] +
+                         [(k, c) for k in range(4, 10) for c in ([1, 0, 2], [63, 64, 0, 65], [300, 5, 130])])
+@pytest.mark.parametrize("k,n", [(16, 16), (64, 7), (300, 96), (512, 260), (1040, 129), (2320, 520)])
+def test_every_kernel(kernel, which, counts, k, n):
+    kernel(which)
+    g = np.random.default_rng(which)
+    index = g.integers(-1, 50, size=sum(counts) + 2)
+    for dtype, pads, offset, between, idx in (("bf16", (0, 0, 0), 0, 0, None), ("f32", (16, 32, 4), 0, 16, index), ("f16", (1, 2, 3), 3, 5, index), ("f32", (0, 0, 0), 0, 0, index)):
+        extra = dict(pads=pads, offset=offset, between=between, index=idx, x_rows=None if idx is None else 50, behind=2)
+        run(counts, k, n, dtype, "gelu", seed=which, **extra)
+        run(counts, k, n, dtype, "silu", gated=True, seed=which + 10, **extra)
+
+
+@pytest.mark.parametrize("k", [1024, 1025, 2047, 2048, 4096, 4111, 8192, 8208, 16384, 16399, 32768, 32780])
+def test_depths_of_single_tokens(k):
+    run([1, 0, 1, 1], k, 21, "f32", seed=k)
+    run([0, 1, 1, 0], k, 5, "bf16", "silu", gated=True, index=np.array([1, 0]), seed=k)
