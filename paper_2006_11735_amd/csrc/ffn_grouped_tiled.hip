@@ -36,6 +36,13 @@ static hipError_t launch_tiles(const GroupedArgs &a, hipStream_t st)
     return a.l.w2 ? launch_one<TN, TM, WN, WM, BK, 2, true, false>(a, st) : launch_one<TN, TM, WN, WM, BK, 2, false, false>(a, st);
 }
 
+template <int TN, int TM, int WN, int WM, int BK, int STAGES>
+static hipError_t launch_direct(const GroupedArgs &a, hipStream_t st)
+{
+    if (!tiled_direct(a.l, a.expert_stride)) return launch_tiles<2, 2, 4, 2, 128, 3>(a, st);
+    return a.l.w2 ? launch_one<TN, TM, WN, WM, BK, STAGES, true, true>(a, st) : launch_one<TN, TM, WN, WM, BK, STAGES, false, true>(a, st);
+}
+
 // (the cases in the order of kTiles)
 hipError_t launch_grouped_tiled(const GroupedArgs &a, int tile, hipStream_t st)
 {
@@ -46,6 +53,9 @@ hipError_t launch_grouped_tiled(const GroupedArgs &a, int tile, hipStream_t st)
     case 2: return launch_tiles<2, 2, 2, 2, 128, 2>(a, st);
     case 3: return launch_tiles<2, 2, 2, 2, 128, 4>(a, st);
     case 4: return launch_tiles<2, 1, 2, 2, 128, 3>(a, st);
+    case 6: return launch_direct<4, 2, 2, 2, 64, 3>(a, st);
+    case 7: return launch_direct<2, 4, 2, 2, 64, 3>(a, st);
+    case 8: return launch_direct<2, 2, 2, 2, 64, 4>(a, st);
     default:
         if (a.l.w2) return launch_tiles<2, 1, 1, 2, 128, 4>(a, st);
         return tiled_direct(a.l, a.expert_stride) ? launch_one<1, 1, 2, 2, 128, 4, false, true>(a, st) : launch_one<1, 1, 2, 2, 128, 2, false, false>(a, st);

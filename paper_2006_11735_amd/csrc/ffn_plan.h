@@ -255,6 +255,7 @@ inline GroupedPlan plan_grouped(const GroupedArgs &a, const LinearTuning &tuning
     }
     if (!tiled || (force != 0 && force < 4)) return p;
     p.kernel = LinearKernel::tiled;
+    if (force >= 10) { p.tile = force - 4; return p; }
     float best = 0.f;
     const float steps = (float)((a.l.K + 127) / 128);
     for (int c = 0; c < kTileKinds; ++c) {
@@ -290,5 +291,14 @@ struct LinearS4Args {
     int group, groups;             // numbers of a group (32, 64, 128 or 256), groups of a row
     int act, dtype, scale_dtype;
 };
+
+// Up to four rows token by token, up to 64 by the kernel for few rows
+inline LinearKernel plan_s4(const LinearS4Args &a, const LinearTuning &tuning)
+{
+    const int force = tuning.kernel;
+    if (a.M <= 4 && a.K >= 16 && a.K <= 32768 && (force == 0 || force == 2)) return LinearKernel::tokens;
+    if (a.M <= 64 && a.K >= 16 && (force == 0 || force == 3)) return LinearKernel::few;
+    return LinearKernel::plain;
+}
 
 }  // namespace icnn

@@ -19,6 +19,32 @@ __device__ __forceinline__ v4i sixteen_of(const v4i &block)
 // Scale i: its number as it is, and over 16 (exact, but for numbers that leave float32 downwards) for the sums of sixteen_of's numbers
 __device__ __forceinline__ float group_scale(const void *p, long long i, int dtype) { return load_number(p, i, dtype) * 0.0625f; }
 
+__device__ __forceinline__ float scale_of(uint32_t bits, int dtype) { return value_of(bits, dtype) * 0.0625f; }
+
+// Bits of scale i, two bytes or four
+template <bool WIDE>
+__device__ __forceinline__ uint32_t scale_bits(const void *p, long long i)
+{
+    return WIDE ? ((const uint32_t *)p)[i] : ((const uint16_t *)p)[i];
+}
+
+// Numbers k .. k + 15 of a row of K >= 16 in two steps, so that no load hangs on a condition: sixteen that are there, and of those what k asks for, zeros behind
+// the row's end (left: numbers from k on)
+__device__ __forceinline__ v4i load_there(const int8_t *row, int k, int K) { return *(const v4i_any *)(row + min(k, K - 16)); }
+
+__device__ __forceinline__ v4i put_right(v4i v, int left)
+{
+    if (left <= 0) return v4i{};
+    if (left >= 16) return v;
+    const int by = 16 - left;                              // bytes in front that belong to the piece before
+    if (by & 8) v = v4i{v[2], v[3], 0, 0};
+    if (by & 4) v = v4i{v[1], v[2], v[3], 0};
+    v4i r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = (int)__builtin_amdgcn_alignbyte(i < 3 ? v[i + 1] : 0, v[i], by & 3);
+    return r;
+}
+
 // Outputs n .. n + 3 of row m from their sums over the groups
 template <bool GATED>
 __device__ __forceinline__ void finish_four_s4(const LinearS4Args &a, const float (&s)[4], const float (&s2)[4], int m, int n)
@@ -36,5 +62,8 @@ __device__ __forceinline__ void finish_four_s4(const LinearS4Args &a, const floa
             store_number(a.y, m * a.ldy + n + e, a.dtype, v[e]);
         }
 }
+
+hipError_t launch_tokens_s4(const LinearS4Args &a, hipStream_t st);
+hipError_t launch_few_s4(const LinearS4Args &a, hipStream_t st);
 
 }  // namespace icnn

@@ -60,6 +60,11 @@ static void launch_plain(const LinearS4Args &a, hipStream_t st)
 
 hipError_t launch_linear_s4(const LinearS4Args &a, hipStream_t st)
 {
+    switch (plan_s4(a, linear_tuning())) {
+    case LinearKernel::tokens: return launch_tokens_s4(a, st);
+    case LinearKernel::few: return launch_few_s4(a, st);
+    default: break;
+    }
     if (a.w2) launch_plain<true>(a, st);
     else launch_plain<false>(a, st);
     return hipGetLastError();

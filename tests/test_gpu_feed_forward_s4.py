@@ -189,6 +189,28 @@ def test_on_another_stream_and_replayed(rows):
         assert torch.equal(y, want), i
 
 
+@pytest.fixture
+def kernel():
+    yield lambda k: B.icnn_set_tuning("ff_kernel", k)
+    B.icnn_set_tuning("reset")
+
+
+@pytest.mark.parametrize("which,rows", [(1, 1), (1, 50), (2, 1), (2, 2), (2, 3), (2, 4), (3, 1), (3, 16), (3, 17), (3, 33), (3, 64)])
+@pytest.mark.parametrize("k,n", [(16, 16), (64, 7), (300, 96), (512, 260), (1040, 129), (2320, 520)])
+def test_every_kernel(kernel, which, rows, k, n):
+    kernel(which)
+    for dtype, pads, offset, group, scales in (("bf16", (0, 0, 0), 0, 128, "f16"), ("f32", (16, 4, 8), 0, 64, "f32"), ("f16", (1, 3, 4), 3, 256, "bf16"), ("f32", (0, 0, 0), 0, 32, "f16")):
+        run(rows, k, n, group, dtype, "gelu", residual=True, pads=pads, offset=offset, scales=scales, seed=which)
+        run(rows, k, n, group, dtype, "silu", gated=True, pads=pads, offset=offset, scales=scales, seed=which + 10)
+
+
+@pytest.mark.parametrize("k", [2047, 2048, 2049, 4095, 4096, 4111, 8192, 8208, 16384, 16399, 32767, 32768, 32780])
+def test_depths_of_single_tokens(k):
+    for rows in (1, 2, 4):
+        run(rows, k, 21, 128, "f32", residual=True, seed=k)
+        run(rows, k, 5, 32, "bf16", "silu", gated=True, seed=k)
+
+
 # ---- weights to 4 bits
 
 @pytest.mark.parametrize("group", [32, 64, 128, 256])
