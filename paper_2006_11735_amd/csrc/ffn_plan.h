@@ -292,13 +292,24 @@ struct LinearS4Args {
     int act, dtype, scale_dtype;
 };
 
-// Up to four rows token by token, up to 64 by the kernel for few rows
-inline LinearKernel plan_s4(const LinearS4Args &a, const LinearTuning &tuning)
+// Tiles of a product with 4-bit weights: {rows, weight rows}
+constexpr int kS4Tiles[][2] = {{128, 256}, {128, 128}, {64, 32}};
+constexpr int kS4TileKinds = sizeof(kS4Tiles) / sizeof(kS4Tiles[0]);
+
+struct S4Plan {
+    LinearKernel kernel;
+    int tile;                      // of LinearKernel::tiled: its place in kS4Tiles
+};
+
+// Up to four rows token by token, up to 32 by the kernel for few rows, the others in tiles; k below 16 and rows gigabytes apart by the plain kernel
+inline S4Plan plan_s4(const LinearS4Args &a, const LinearTuning &tuning)
 {
     const int force = tuning.kernel;
-    if (a.M <= 4 && a.K >= 16 && a.K <= 32768 && (force == 0 || force == 2)) return LinearKernel::tokens;
-    if (a.M <= 64 && a.K >= 16 && (force == 0 || force == 3)) return LinearKernel::few;
-    return LinearKernel::plain;
+    if (a.M <= 4 && a.K >= 16 && a.K <= 32768 && (force == 0 || force == 2)) return {LinearKernel::tokens, 0};
+    if (a.M <= 32 && a.K >= 16 && (force == 0 || force == 3)) return {LinearKernel::few, 0};
+    if (a.K < 16 || a.ldx > (1 << 22) || (force != 0 && force < 4)) return {LinearKernel::plain, 0};
+    if (force >= 4) return {LinearKernel::tiled, force - 4 < kS4TileKinds ? force - 4 : kS4TileKinds - 1};
+    return {LinearKernel::tiled, 0};
 }
 
 }  // namespace icnn

@@ -65,5 +65,10 @@ __device__ __forceinline__ void finish_four_s4(const LinearS4Args &a, const floa
 
 hipError_t launch_tokens_s4(const LinearS4Args &a, hipStream_t st);
 hipError_t launch_few_s4(const LinearS4Args &a, hipStream_t st);
+// (a file for each size of a group: they take long to compile)
+hipError_t launch_tiled_s4_32(const LinearS4Args &a, int tile, hipStream_t st);
+hipError_t launch_tiled_s4_64(const LinearS4Args &a, int tile, hipStream_t st);
+hipError_t launch_tiled_s4_128(const LinearS4Args &a, int tile, hipStream_t st);
+hipError_t launch_tiled_s4_256(const LinearS4Args &a, int tile, hipStream_t st);
 
 }  // namespace icnn

@@ -60,10 +60,18 @@ static void launch_plain(const LinearS4Args &a, hipStream_t st)
 
 hipError_t launch_linear_s4(const LinearS4Args &a, hipStream_t st)
 {
-    switch (plan_s4(a, linear_tuning())) {
+    const S4Plan plan = plan_s4(a, linear_tuning());
+    switch (plan.kernel) {
     case LinearKernel::tokens: return launch_tokens_s4(a, st);
     case LinearKernel::few: return launch_few_s4(a, st);
-    default: break;
+    case LinearKernel::tiled:
+        switch (a.group) {
+        case 32: return launch_tiled_s4_32(a, plan.tile, st);
+        case 64: return launch_tiled_s4_64(a, plan.tile, st);
+        case 128: return launch_tiled_s4_128(a, plan.tile, st);
+        default: return launch_tiled_s4_256(a, plan.tile, st);
+        }
+    case LinearKernel::plain: break;
     }
     if (a.w2) launch_plain<true>(a, st);
     else launch_plain<false>(a, st);
