@@ -292,8 +292,14 @@ struct LinearS4Args {
     int act, dtype, scale_dtype;
 };
 
-// Tiles of a product with 4-bit weights: {rows, weight rows}
-constexpr int kS4Tiles[][2] = {{128, 256}, {128, 128}, {64, 32}};
+// Tiles of a product with 4-bit weights, one on a compute unit at a time: {rows, weight rows, us that do not depend on k, us for 128 numbers of k in groups of 32, of 64 and of
+// 128 or 256}.  Measured with 8192 -> 8192: 1024 rows by the first 84 us (by the second 98), 512 by the second 50 (84), 64 by the third 19 (46); in groups of 32 1024
+// rows 156 us (177)
+struct S4TileCost {
+    int m, n;
+    float fixed, step[3];
+};
+constexpr S4TileCost kS4Tiles[] = {{128, 256, 9.f, {2.3f, 1.5f, 1.17f}}, {128, 128, 9.f, {1.25f, 0.8f, 0.64f}}, {64, 32, 4.f, {0.28f, 0.23f, 0.21f}}};
 constexpr int kS4TileKinds = sizeof(kS4Tiles) / sizeof(kS4Tiles[0]);
 
 struct S4Plan {
@@ -301,7 +307,8 @@ struct S4Plan {
     int tile;                      // of LinearKernel::tiled: its place in kS4Tiles
 };
 
-// Up to four rows token by token, up to 32 by the kernel for few rows, the others in tiles; k below 16 and rows gigabytes apart by the plain kernel
+// Up to four rows token by token (1 x 16384 -> 4096: 8.3 us, by the kernel for few rows 16), up to 32 by the kernel for few rows (24 x 8192 -> 8192: 15 us, in tiles 19),
+// the others in tiles; k below 16 and rows gigabytes apart by the plain kernel
 inline S4Plan plan_s4(const LinearS4Args &a, const LinearTuning &tuning)
 {
     const int force = tuning.kernel;
@@ -309,7 +316,21 @@ inline S4Plan plan_s4(const LinearS4Args &a, const LinearTuning &tuning)
     if (a.M <= 32 && a.K >= 16 && (force == 0 || force == 3)) return {LinearKernel::few, 0};
     if (a.K < 16 || a.ldx > (1 << 22) || (force != 0 && force < 4)) return {LinearKernel::plain, 0};
     if (force >= 4) return {LinearKernel::tiled, force - 4 < kS4TileKinds ? force - 4 : kS4TileKinds - 1};
-    return {LinearKernel::tiled, 0};
+    const int steps = (a.K + 127) / 128, by_group = a.group == 32 ? 0 : a.group == 64 ? 1 : 2;
+    S4Plan p = {LinearKernel::tiled, 0};
+    float best = 0.f;
+    for (int c = 0; c < kS4TileKinds; ++c) {
+        const S4TileCost &t = kS4Tiles[c];
+        // (the last one's weight rows are twice as many in a gated layer, for a third more time)
+        const bool wider = c == kS4TileKinds - 1 && a.w2;
+        const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + (wider ? 2 : 1) * t.n - 1) / ((wider ? 2 : 1) * t.n));
+        const float us = __builtin_ceilf(tiles / 256.f) * (t.fixed + (wider ? 1.3f : 1.f) * (float)steps * t.step[by_group]);
+        if (best == 0.f || us < best) {
+            best = us;
+            p.tile = c;
+        }
+    }
+    return p;
 }
 
 }  // namespace icnn

@@ -20,34 +20,68 @@ long long chunk_of(long long rows)
     return per < kMostChunk ? per : kMostChunk;
 }
 
-// Logits as numbers that are ordered as they are: 0 for what is never chosen (minus infinity, places behind the last expert), all ones for a NaN
-__device__ __forceinline__ uint32_t key_of(float v)
+// Logits as numbers that are ordered as they are, of which 0 is never chosen (minus infinity, places behind the last expert).  A 16-bit logit leaves room for its expert,
+// counted from above: the numbers of a row are all different then, and the largest of equal logits is the lowest expert's.
+template <int DT>
+__device__ __forceinline__ uint32_t key_of(uint32_t bits, int e)
 {
-    const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.f);          // (minus zero is zero)
-    const uint32_t key = b ^ (b >> 31 ? ~0u : 0x80000000u);
-    return v != v ? ~0u : v == -__builtin_huge_valf() ? 0 : key;
+    const float v = value_of(bits, DT);
+    if (v == -__builtin_huge_valf()) return 0;
+    if constexpr (DT == kF32) {
+        const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.f);      // (minus zero is zero)
+        return v != v ? ~0u : b ^ (b >> 31 ? ~0u : 0x80000000u);
+    } else {
+        const uint32_t b = v == 0.f ? 0 : bits, key = v != v ? 0xffffu : b ^ (b >> 15 ? 0xffffu : 0x8000u);
+        return key << 16 | (0xffffu - (uint32_t)e);
+    }
 }
 
+template <int DT>
 __device__ __forceinline__ float value_of_key(uint32_t key)
 {
-    if (key == ~0u) return __builtin_nanf("");
-    return __builtin_bit_cast(float, key ^ (key >> 31 ? 0x80000000u : ~0u));
+    if constexpr (DT == kF32) {
+        return key == ~0u ? __builtin_nanf("") : __builtin_bit_cast(float, key ^ (key >> 31 ? 0x80000000u : ~0u));
+    } else {
+        const uint32_t k = key >> 16;
+        return k == 0xffffu ? __builtin_nanf("") : value_of(k ^ (k >> 15 ? 0x8000u : 0xffffu), DT);
+    }
 }
 
+// f over LANES lanes next to each other, in all of them
 template <int LANES, class F>
-__device__ __forceinline__ auto over_lanes(decltype(F{}(0, 0)) v, F f)
+__device__ __forceinline__ uint32_t over_lanes(uint32_t v, F f)
 {
-#pragma unroll
-    for (int d = LANES / 2; d; d >>= 1) v = f(v, __shfl_xor(v, d));
+    static_assert(LANES >= 16 && LANES <= 64, "rows of sixteen lanes");
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));          // lanes ^ 1
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));          // lanes ^ 2
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));         // eight lanes mirrored
+    v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));         // sixteen lanes mirrored
+    if (LANES >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = f(r[0], r[1]);
+    }
+    if (LANES == 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = f(r[0], r[1]);
+    }
     return v;
 }
 
-struct MaxU {
+struct Largest {
     __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
 };
-struct SumF {
-    __device__ float operator()(float a, float b) const { return a + b; }
+struct Least {
+    __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a < b ? a : b; }
 };
+struct Sum {
+    __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b)); }
+};
+
+template <int LANES>
+__device__ __forceinline__ float sum_over(float v)
+{
+    return __builtin_bit_cast(float, over_lanes<LANES>(__builtin_bit_cast(uint32_t, v), Sum{}));
+}
 
 // Exclusive sums of `experts` counts in LDS, by all threads of the workgroup; the total is returned
 template <int THREADS>
@@ -87,18 +121,16 @@ __device__ __forceinline__ int scan_counts(int *counts, int *first, int experts)
 
 }  // namespace
 
-// LANES lanes a token with P experts each, next to each other: among equal ones the lowest lane's first has the lowest index.  ONE: all rows are this workgroup's, which
-// then places them too.
-template <int LANES, int P, bool ONE>
+// LANES lanes a token with P experts each, next to each other.  ONE: all rows are this workgroup's, which then places them too.
+template <int LANES, int P, int DT, bool ONE>
 __global__ __launch_bounds__(256) void route_choose_kernel(const RouteArgs a, int chunk)
 {
     constexpr int TOKENS = 256 / LANES;                    // at a time
     __shared__ uint32_t mask[kMostExperts];
     __shared__ int counts[kMostExperts], first[ONE ? kMostExperts : 1];
-    const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
+    const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES, e0 = lane * P;
     const long long begin = (long long)blockIdx.x * chunk;
     const int mine = (int)min((long long)chunk, a.rows - begin);
-    const unsigned long long own_lanes = (LANES == 64 ? ~0ull : (1ull << LANES) - 1) << (threadIdx.x & 63) / LANES * LANES;
     for (int e = threadIdx.x; e < a.experts; e += 256) {
         mask[e] = 0;
         counts[e] = 0;
@@ -109,45 +141,56 @@ __global__ __launch_bounds__(256) void route_choose_kernel(const RouteArgs a, in
         for (int at = base; at < min(base + kMask, mine); at += TOKENS) {
             const bool some = at + slot < min(base + kMask, mine);
             const long long t = begin + at + (some ? slot : 0);
-            uint32_t key[P], best = 0;
+            uint32_t key[P], bits[P], best = 0;
+            if (P % 8 == 0 && a.experts == LANES * P) {
+#pragma unroll
+                for (int i = 0; i < P / 8; ++i) {
+                    const Eight<DT> v = load_eight<DT>(a.logits, t * a.ld + e0 + 8 * i);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) bits[(8 * i + q) % P] = DT == kF32 ? (uint32_t)v.b[DT == kF32 ? q >> 2 : 0][q & 3] : (uint32_t)v.b[0][q >> 1] >> (16 * (q & 1)) & 0xffffu;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < P; ++i) bits[i] = load_bits(a.logits, t * a.ld + min(e0 + i, a.experts - 1), DT);
+            }
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                const int e = lane * P + i;
-                const float v = load_number(a.logits, t * a.ld + min(e, a.experts - 1), a.dtype);
-                key[i] = e < a.experts ? key_of(v) : 0;
+                key[i] = e0 + i < a.experts ? key_of<DT>(bits[i], e0 + i) : 0;
                 best = max(best, key[i]);
             }
-            const uint32_t largest = over_lanes<LANES>(best, MaxU{});
-            const float most = value_of_key(largest);
+            const uint32_t largest = over_lanes<LANES>(best, Largest{});
+            const float most = value_of_key<DT>(largest);
             float every = 0.f;
             if (a.score == 0 && !a.normalise) {
 #pragma unroll
-                for (int i = 0; i < P; ++i) every += key[i] ? expf(value_of_key(key[i]) - most) : 0.f;
-                every = over_lanes<LANES>(every, SumF{});
+                for (int i = 0; i < P; ++i) every += key[i] ? expf(value_of_key<DT>(key[i]) - most) : 0.f;
+                every = sum_over<LANES>(every);
             }
-            uint32_t chosen = 0;                           // lane j has the token's choice j
+            uint32_t chosen = 0, m = largest;              // lane j has the token's choice j
             int which = -1;
             for (int j = 0; j < a.top; ++j) {
-                const uint32_t m = over_lanes<LANES>(best, MaxU{});
-                const unsigned long long has = __ballot(best == m && m != 0) & own_lanes;
-                const int winner = has ? __builtin_ctzll(has) : -1;
-                int hit = -1;
-                uint32_t next = 0;
+                uint32_t e;
+                if constexpr (DT == kF32) {                // the lowest of those that have it
+                    uint32_t lowest = ~0u;
+#pragma unroll
+                    for (int i = P - 1; i >= 0; --i) lowest = key[i] == m ? e0 + i : lowest;
+                    e = over_lanes<LANES>(lowest, Least{});
+                } else {
+                    e = 0xffffu - (m & 0xffffu);
+                }
+                if (lane == j && m) {
+                    chosen = m;
+                    which = (int)e;
+                }
+                best = 0;
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
-                    const bool takes = winner == (int)(threadIdx.x & 63) && hit < 0 && key[i] == m;
-                    hit = takes ? i : hit;
-                    key[i] = takes ? 0 : key[i];
-                    next = max(next, key[i]);
+                    key[i] = (DT == kF32 ? e == (uint32_t)(e0 + i) : key[i] == m) ? 0 : key[i];
+                    best = max(best, key[i]);
                 }
-                best = next;
-                const int e = __shfl(lane * P + hit, winner < 0 ? 0 : winner);
-                if (lane == j && winner >= 0) {
-                    chosen = m;
-                    which = e;
-                }
+                m = over_lanes<LANES>(best, Largest{});
             }
-            const float l = value_of_key(chosen);
+            const float l = value_of_key<DT>(chosen);
             float g;
             if (a.score == 0) {
                 g = which >= 0 ? expf(l - most) : 0.f;
@@ -156,7 +199,7 @@ __global__ __launch_bounds__(256) void route_choose_kernel(const RouteArgs a, in
                 const float shift = a.normalise && most < 0.f ? most : 0.f;
                 g = which < 0 ? 0.f : l > 0.f ? 1.f / (1.f + expf(-l)) : expf(l - shift) / (1.f + expf(l));
             }
-            const float sum = a.normalise ? over_lanes<LANES>(g, SumF{}) : a.score == 0 ? every : 1.f;
+            const float sum = a.normalise ? sum_over<LANES>(g) : a.score == 0 ? every : 1.f;
             if (some && lane < a.top) {
                 a.expert[t * a.top + lane] = which;
                 a.gate[t * a.top + lane] = which >= 0 ? g / sum * a.scale : 0.f;
@@ -190,7 +233,7 @@ __global__ __launch_bounds__(256) void route_choose_kernel(const RouteArgs a, in
             a.place[i] = p;
         }
     } else {
-        for (int e = threadIdx.x; e < a.experts; e += 256) a.counts[(long long)blockIdx.x * a.experts + e] = (uint16_t)counts[e];
+        for (int e = threadIdx.x; e < a.experts; e += 256) a.counts[(long long)blockIdx.x * ((a.experts + 7) / 8 * 8) + e] = (uint16_t)counts[e];
     }
 }
 
@@ -207,17 +250,26 @@ __global__ __launch_bounds__(1024) void route_place_kernel(const RouteArgs a, in
         total[e] = before[e] = 0;
     }
     __syncthreads();
-    // 1024 / experts threads an expert, each every so many-th chunk
-    const int ways = 1024 / a.experts, e0 = t % a.experts, way = t / a.experts;
+    // Eight experts a thread, of every so many-th chunk: a chunk's counts are in whole 16 bytes (256 chunks of 256 experts: eight loads a thread, one by one 64)
+    const int pieces = (a.experts + 7) / 8, ways = 1024 / pieces, piece = t % pieces, way = t / pieces;
     if (way < ways) {
-        int all = 0, low = 0;
+        int all[8] = {}, low[8] = {};
+#pragma unroll 4
         for (int q = way; q < chunks; q += ways) {
-            const int v = a.counts[(long long)q * a.experts + e0];
-            all += v;
-            low += q < (int)blockIdx.x ? v : 0;
+            const v4i v = *((const v4i *)a.counts + (long long)q * pieces + piece);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int n = (int)((uint32_t)v[e >> 1] >> (16 * (e & 1)) & 0xffffu);
+                all[e] += n;
+                low[e] += q < (int)blockIdx.x ? n : 0;
+            }
         }
-        atomicAdd(&total[e0], all);
-        atomicAdd(&before[e0], low);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (8 * piece + e < a.experts) {
+                atomicAdd(&total[8 * piece + e], all[e]);
+                atomicAdd(&before[8 * piece + e], low[e]);
+            }
     }
     __syncthreads();
     const int sum = scan_counts<1024>(total, first, a.experts);
@@ -255,22 +307,28 @@ size_t route_workspace(long long rows, int experts)
 {
     if (rows <= kMask) return 0;
     const long long chunk = chunk_of(rows);
-    return (size_t)((rows + chunk - 1) / chunk) * (size_t)experts * 2;
+    return (size_t)((rows + chunk - 1) / chunk) * (size_t)((experts + 7) / 8) * 16;
+}
+
+template <int LANES, int P, int DT>
+static hipError_t launch_of(const RouteArgs &a, hipStream_t st)
+{
+    if (a.rows <= kMask) {
+        hipLaunchKernelGGL((route_choose_kernel<LANES, P, DT, true>), dim3(1), dim3(256), 0, st, a, kMask);
+        return hipGetLastError();
+    }
+    const long long chunk = chunk_of(a.rows);
+    const unsigned chunks = (unsigned)((a.rows + chunk - 1) / chunk);
+    hipLaunchKernelGGL((route_choose_kernel<LANES, P, DT, false>), dim3(chunks), dim3(256), 0, st, a, (int)chunk);
+    if (hipError_t e = hipGetLastError()) return e;
+    hipLaunchKernelGGL(route_place_kernel, dim3(chunks), dim3(1024), 0, st, a, (int)chunk);
+    return hipGetLastError();
 }
 
 template <int LANES, int P>
 static hipError_t launch_choose(const RouteArgs &a, hipStream_t st)
 {
-    if (a.rows <= kMask) {
-        hipLaunchKernelGGL((route_choose_kernel<LANES, P, true>), dim3(1), dim3(256), 0, st, a, kMask);
-        return hipGetLastError();
-    }
-    const long long chunk = chunk_of(a.rows);
-    const unsigned chunks = (unsigned)((a.rows + chunk - 1) / chunk);
-    hipLaunchKernelGGL((route_choose_kernel<LANES, P, false>), dim3(chunks), dim3(256), 0, st, a, (int)chunk);
-    if (hipError_t e = hipGetLastError()) return e;
-    hipLaunchKernelGGL(route_place_kernel, dim3(chunks), dim3(1024), 0, st, a, (int)chunk);
-    return hipGetLastError();
+    return a.dtype == kF32 ? launch_of<LANES, P, kF32>(a, st) : a.dtype == kF16 ? launch_of<LANES, P, kF16>(a, st) : launch_of<LANES, P, kBf16>(a, st);
 }
 
 hipError_t launch_route(const RouteArgs &a, hipStream_t st)

@@ -30,9 +30,11 @@ __device__ __forceinline__ int row_key(int q)
 
 template <int TN, int TM, int WN, int WM, int WK, int GROUP, bool GATED>
 struct S4Tile {
-    static constexpr int NW = WN * WM * WK, THREADS = NW * 64, BN = 32 * TN * WN, BM = 32 * TM * WM, XR = 128 * WK, WR = 64 * WK, STAGES = 3, STAGE = BM * XR + BN * WR;
-    static constexpr int STEPS = WK == 1 ? 4 : 1, GROUPS = XR * STEPS / GROUP;     // of a chunk of scales, which come in together
-    static constexpr int SCALES = GROUPS * BN * 4, LDS = STAGES * STAGE + 2 * SCALES + BM * 4, OUT = GATED ? BN / 2 : BN;
+    static constexpr int NW = WN * WM * WK, THREADS = NW * 64, BN = 32 * TN * WN, BM = 32 * TM * WM, XR = 128 * WK, WR = 64 * WK, STAGE = BM * XR + BN * WR;
+    static constexpr int STEPS = WK == 1 ? (GROUP == 32 ? 2 : 4) : 1, GROUPS = XR * STEPS / GROUP;       // of a chunk of scales, which come in together
+    static constexpr int SCALES = GROUPS * BN * 4, REST = 2 * SCALES + BM * 4, STAGES = 4 * STAGE + REST <= 163840 ? 4 : 3, LDS = STAGES * STAGE + REST;
+    static constexpr bool AHEAD = STAGES == 4;             // fragments of the next stage under this one's products
+    static constexpr int OUT = GATED ? BN / 2 : BN;
     static_assert(WM * 32 * OUT * 4 <= STAGES * STAGE && (WK - 1) * BM * BN * 4 <= STAGES * STAGE && LDS <= 163840, "what takes the ring's place");
 };
 
@@ -82,6 +84,7 @@ __global__ __launch_bounds__(WN * WM * WK * 64, 2) void s4_tiled_kernel(const Li
         off_x[j] = (unsigned)min(q, a.M - 1 - m0) * (unsigned)a.ldx + (DIRECT ? piece_x[j] : 0);
     }
     const int steps = (a.K + XR - 1) / XR;
+    // (no branch on whether a row ends in the step: behind one the compiler no longer counts the copies in flight and waits for them where it waits for the scales)
     auto copy = [&](int s) {
         uint8_t *const to = lds + (s % STAGES) * STAGE + wave * 1024;
         const int left_w = (int)a.ldw - s * WR, left_x = a.K - s * XR;
@@ -112,24 +115,24 @@ __global__ __launch_bounds__(WN * WM * WK * 64, 2) void s4_tiled_kernel(const Li
         for (int j = 0; j < LX; ++j) *(v4i *)(to + j * NW * 1024) = held[j];
     };
 
-    // ---- scales: chunk c's are [group][weight row] in LDS, the next one's come in part by part under its steps.  Element e of a chunk is row e / GROUPS's of group
-    // e % GROUPS: lanes next to each other read groups next to each other
-    constexpr int PART = GROUPS * BN / STEPS, EACH = (PART + S::THREADS - 1) / S::THREADS;
-    constexpr bool WHOLE = PART % S::THREADS == 0;
+    // ---- scales: chunk c's are [group][weight row] in LDS, the next one's on their way.  Element e of a chunk is row e / GROUPS's of group e % GROUPS: lanes next to each
+    // other read groups next to each other
+    constexpr int EACH = (GROUPS * BN + S::THREADS - 1) / S::THREADS;
+    constexpr bool WHOLE = GROUPS * BN % S::THREADS == 0;
     uint32_t bits[EACH];
-    auto fetch_scales = [&](int c, int part) {
+    auto fetch_scales = [&](int c) {
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const int e = part * PART + (WHOLE ? i * S::THREADS + t : min(i * S::THREADS + t, PART - 1)), q = e / GROUPS;
+            const int e = WHOLE ? i * S::THREADS + t : min(i * S::THREADS + t, GROUPS * BN - 1), q = e / GROUPS;
             const long long n = min(n0 + of_row(q), a.N - 1);
             bits[i] = scale_bits<WIDE>(second(q) ? a.ws2 : a.ws, n * a.groups + min(c * GROUPS + e % GROUPS, a.groups - 1));
         }
     };
-    auto put_scales = [&](int c, int part) {
+    auto put_scales = [&](int c) {
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const int e = part * PART + i * S::THREADS + t;
-            if (WHOLE || i * S::THREADS + t < PART)
+            const int e = i * S::THREADS + t;
+            if (WHOLE || e < GROUPS * BN)
                 scales[((c & 1) * GROUPS + e % GROUPS) * BN + e / GROUPS] = c * GROUPS + e % GROUPS < a.groups ? scale_of(bits[i], a.scale_dtype) : 0.f;
         }
     };
@@ -140,105 +143,128 @@ __global__ __launch_bounds__(WN * WM * WK * 64, 2) void s4_tiled_kernel(const Li
         asm volatile("" ::: "memory");
     };
 
-    // ---- a stage's products
+    // ---- a stage's products.  A unit is what one scale holds for, 128 numbers at most (a group of 256 is two): a tile of 32 x 32 sums takes `CHAIN` instructions for it,
+    // and then 32 for the scaling, which is done under the next tile's products; the last tile's is under the next stage's.
     const int r = lane & 31, h = lane >> 5;
-    float sum[TN][TM][16] = {};
-    auto products = [&](int s, int in_chunk, int c) {
-        const uint8_t *const xs = lds + (s % STAGES) * STAGE, *const ws = xs + BM * XR;
-        const float *const at = scales + (c & 1) * GROUPS * BN + wn * TN * 32 + r;
-        auto rows = [&](int j, int piece) {
-            const int q = (wm * TM + j) * 32 + r;
-            return *(const v4i *)(xs + q * XR + (((wk * 8 + piece) ^ row_key<XR>(q)) << 4));
-        };
-        auto block = [&](int i, int b) {
-            const int q = (wn * TN + i) * 32 + r;
-            return *(const v4i *)(ws + q * WR + (((wk * 4 + b) ^ row_key<WR>(q)) << 4));
-        };
-        const int group0 = (in_chunk * WK + wk) * 128 / GROUP;
-        auto scaled = [&](float(&to)[16], const v16i &acc, float scale) {
+    constexpr int NUMBERS = GROUP < 128 ? GROUP : 128, UNITS = 128 / NUMBERS, CHAIN = NUMBERS / 32, TILES = UNITS * TN * TM, RAW = GROUP == 32 ? 1 : CHAIN / 2;
+    typedef float v16f __attribute__((ext_vector_type(16)));
+    v16f sum[TN][TM] = {};
+    v16i last = {};                                        // the last tile's sums of the stage before, and their scale
+    float behind = 0.f;
+    v4i x[TM][CHAIN], raw[TN][RAW];
+    float scale[TN];
+    // Fragments of unit u of stage s: of a unit of 32 numbers lane half h has the weights' block's half h, of others the block h of each two, of which first the lower
+    // and then the upper numbers
+    const int row_x = (wm * TM * 32 + r) * XR, row_w = BM * XR + (wn * TN * 32 + r) * WR;         // (32 rows on, the keys are the same)
+    auto load_rows = [&](int j, int s, int u) {
+        const uint8_t *const from = lds + (s % STAGES) * STAGE + j * 32 * XR;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) to[e] += (float)acc[e] * scale;
-        };
-        if constexpr (GROUP == 32) {                       // a block, its halves by the lanes' halves
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                v4i x[TM];
-#pragma unroll
-                for (int j = 0; j < TM; ++j) x[j] = rows(j, 2 * b + h);
-#pragma unroll
-                for (int i = 0; i < TN; ++i) {
-                    const v4i from = block(i, b);
-                    const float scale = at[(group0 + b) * BN + i * 32];
-                    v4i w;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = (int)((unsigned)from[e] << (h ? 0 : 4) & 0xf0f0f0f0u);
-#pragma unroll
-                    for (int j = 0; j < TM; ++j) scaled(sum[i][j], __builtin_amdgcn_mfma_i32_32x32x32_i8(x[j], w, v16i{}, 0, 0, 0), scale);
-                }
-            }
-        } else {                                           // 64 numbers, a block in each half of the lanes: its lower and then its upper numbers
-            constexpr int PAIRS = GROUP == 64 ? 1 : 2;     // of which a unit of the sums is made (a group of 256 is two units)
-#pragma unroll
-            for (int u = 0; u < 2 / PAIRS; ++u) {
-                v4i x[TM][PAIRS][2];
-#pragma unroll
-                for (int j = 0; j < TM; ++j)
-#pragma unroll
-                    for (int p = 0; p < PAIRS; ++p)
-#pragma unroll
-                        for (int f = 0; f < 2; ++f) x[j][p][f] = rows(j, 4 * (u * PAIRS + p) + 2 * h + f);
-#pragma unroll
-                for (int i = 0; i < TN; ++i) {
-                    v4i w[PAIRS][2];
-#pragma unroll
-                    for (int p = 0; p < PAIRS; ++p) {
-                        const v4i from = block(i, 2 * (u * PAIRS + p) + h);
-                        w[p][0] = sixteen_of<false>(from);
-                        w[p][1] = sixteen_of<true>(from);
-                    }
-                    const float scale = at[(group0 + u) * BN + i * 32];
-#pragma unroll
-                    for (int j = 0; j < TM; ++j) {
-                        v16i acc = {};
-#pragma unroll
-                        for (int p = 0; p < PAIRS; ++p)
-#pragma unroll
-                            for (int f = 0; f < 2; ++f) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[j][p][f], w[p][f], acc, 0, 0, 0);
-                        scaled(sum[i][j], acc, scale);
-                    }
-                }
-            }
+        for (int f = 0; f < CHAIN; ++f) {
+            const int piece = wk * 8 + (GROUP == 32 ? 2 * u + h : u * (NUMBERS / 16) + (f >> 1) * 4 + 2 * h + (f & 1));
+            x[j][f] = *(const v4i *)(from + (row_x + ((piece ^ row_key<XR>(r)) << 4)));
         }
     };
-
-    // ---- the stages in turn.  Behind a step's barrier all have done with the stage of the step before: the copies of two steps on go there.
-    if (!DIRECT) {
-        fetch_rows(0);
-        put_rows(0);
-        fetch_rows(1);
-        put_rows(1);
-    }
+    auto load_weights = [&](int i, int s, int u) {
+        const uint8_t *const from = lds + (s % STAGES) * STAGE + i * 32 * WR;
 #pragma unroll
-    for (int u = 0; u < STEPS; ++u) {
-        fetch_scales(0, u);
-        put_scales(0, u);
+        for (int p = 0; p < RAW; ++p) {
+            const int piece = wk * 4 + (GROUP == 32 ? u : u * (NUMBERS / 32) + 2 * p + h);
+            raw[i][p] = *(const v4i *)(from + (row_w + ((piece ^ row_key<WR>(r)) << 4)));
+        }
+    };
+    auto load_scale = [&](int i, int s, int u) {
+        scale[i] = scales[((s / STEPS & 1) * GROUPS + (s % STEPS * WK + wk) * 128 / GROUP + u) * BN + (wn * TN + i) * 32 + r];
+    };
+    auto load_first = [&](int s) {
+#pragma unroll
+        for (int j = 0; j < (TM > 1 ? TM - 1 : 1); ++j) load_rows(j, s, 0);
+#pragma unroll
+        for (int i = 0; i < TN; ++i) load_weights(i, s, 0);
+    };
+    // What a unit's first tile needs is read under the unit before, also that of the stage before if that one's copies can be waited for so early; its last rows under its
+    // own first tile
+    auto products = [&](int s) {
+        asm volatile("s_nop 15\n\ts_nop 3" : "+v"(last));       // (see mfma_drain in conv_common.h: their products are behind the loop's branch)
+        v16i before = last;
+        v4i w[CHAIN];
+        if (!S::AHEAD) load_first(s);
+#pragma unroll
+        for (int q = 0; q < TILES; ++q) {
+            const int u = q / (TN * TM), i = q / TM % TN, j = q % TM;
+            const int next = u + 1 < UNITS ? s : s + 1, unit = u + 1 < UNITS ? u + 1 : 0;
+            const int v = (q + TILES - 1) % TILES;         // the tile before
+            v16f &to = sum[v / TM % TN][v % TM];
+            const float by = q ? scale[v / TM % TN] : behind;
+            if (i == 0 && j == 0 && TM > 1) load_rows(TM - 1, s, u);
+            if (j == 0) {
+#pragma unroll
+                for (int p = 0; p < RAW; ++p) {
+                    if (GROUP == 32) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[0][e] = (int)((unsigned)raw[i][p][e] << (h ? 0 : 4) & 0xf0f0f0f0u);
+                    } else {
+                        w[2 * p] = sixteen_of<false>(raw[i][p]);
+                        w[(2 * p + 1) % CHAIN] = sixteen_of<true>(raw[i][p]);
+                    }
+                }
+                load_scale(i, s, u);
+                if (S::AHEAD || u + 1 < UNITS) load_weights(i, next, unit);
+            }
+            // The empty statements keep the order: an instruction of this tile's, a part of the tile before's sums to scale under it.  Without them the compiler puts
+            // all products first, whose sums are more than there are registers.
+            v16i t = {};
+            asm volatile("" : "+v"(before));
+#pragma unroll
+            for (int f = 0; f < CHAIN; ++f) {
+                t = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[j][f], w[f], t, 0, 0, 0);
+                asm volatile("" : "+v"(t));
+#pragma unroll
+                for (int e = 0; e < 16 / CHAIN; ++e) to[16 / CHAIN * f + e] += (float)before[16 / CHAIN * f + e] * by;
+                asm volatile("" : "+v"(to));
+            }
+            before = t;
+            if (i == TN - 1 && (j < TM - 1 || TM == 1) && (S::AHEAD || u + 1 < UNITS)) load_rows(j, next, unit);
+            __builtin_amdgcn_sched_barrier(0x194);         // (what computes stays in its tile; memory's instructions may move)
+        }
+        last = before;
+        behind = scale[TN - 1];
+    };
+
+    // ---- the stages in turn.  Behind a step's barrier all have done with the stage of the step before: the copies of STAGES - 1 steps on go there.  The step's have
+    // arrived by then (AHEAD: the next one's).
+    if (!DIRECT) {
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s) {
+            fetch_rows(s);
+            put_rows(s);
+        }
     }
-    copy(0);
-    copy(1);
+    fetch_scales(0);
+    put_scales(0);
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) copy(s);
     for (int i = t; i < BM; i += S::THREADS) row_scales[i] = a.xs[min(m0 + i, a.M - 1)];
+    if (S::AHEAD) {
+        FFN_WAIT_VMCNT((STAGES - 2) * COPIES);
+        barrier();
+        load_first(0);
+    }
 #pragma unroll 1
     for (int s = 0; s < steps; ++s) {
         const int c = s / STEPS, part = s % STEPS;
-        FFN_WAIT_VMCNT(COPIES);                            // (the next step's are still in flight; others that are make this wait for more)
+        FFN_WAIT_VMCNT((S::AHEAD ? STAGES - 3 : STAGES - 2) * COPIES);     // (later ones are still in flight; others that are make this wait for more)
         barrier();
-        fetch_scales(c + 1, part);
-        if (!DIRECT) fetch_rows(s + 2);
-        copy(s + 2);
-        products(s, part, c);
-        if (!DIRECT) put_rows(s + 2);
-        put_scales(c + 1, part);
+        if (part == 0) fetch_scales(c + 1);
+        if (!DIRECT) fetch_rows(s + STAGES - 1);
+        copy(s + STAGES - 1);
+        products(s);
+        if (!DIRECT) put_rows(s + STAGES - 1);
+        if (part == STEPS - 1) put_scales(c + 1);
     }
     FFN_WAIT_VMCNT(0);
+    asm volatile("s_nop 15\n\ts_nop 3" : "+v"(last));
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum[TN - 1][TM - 1][e] += (float)last[e] * behind;
 
     // ---- sums of one k range, by the waves of the first one
     barrier();

@@ -239,6 +239,15 @@ def test_choices_without_a_place_add_nothing():
     combine(4, 2, 40, "f32", place=np.full((4, 2), -1), v_rows=1)
 
 
+def test_no_rows_of_v():
+    res = torch.randn((3, 20), device="cuda:0")
+    y = torch.zeros((3, 20), device="cuda:0")
+    B.icombine_rows(B.combine_desc(rows=3, top=2, c=20, v_rows=0, dtype=B.ICNN_F32), None, torch.ones((3, 2), device="cuda:0"),
+                    torch.zeros((3, 2), dtype=torch.int32, device="cuda:0"), res, y)
+    torch.cuda.synchronize()
+    assert torch.equal(y, res)
+
+
 def test_a_gate_that_is_nan_and_rows_that_are_not_read():
     v = torch.full((6, 16), float("nan"), device="cuda:0")
     v[2] = 3.0
