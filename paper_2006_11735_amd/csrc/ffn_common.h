@@ -30,7 +30,7 @@ struct RouteArgs {
     const void *logits;
     int32_t *expert, *place, *token, *offsets;
     float *gate;
-    uint16_t *counts;               // [chunks][experts, in whole eights] of a workspace; null where one chunk has all rows
+    void *counts;                   // [chunks][experts, in whole 16 bytes] of a workspace; null where one chunk has all rows
     long long rows, ld;
     int experts, top, dtype, score, normalise;
     float scale;

@@ -9,51 +9,79 @@ struct Place {
     int expert, m0, end;
 };
 
-// Groups of ROWS positions that there are
-template <int ROWS>
-__device__ __forceinline__ int groups_of(const GroupedArgs &g)
+// Groups of ROWS positions of one expert each: all of them (the last one of an expert may have fewer), or those with more than half of ROWS, or an expert's rest of up to
+// half of ROWS
+enum Groups { kAll, kWholeOrMost, kRest };
+
+template <int ROWS, Groups KIND>
+__device__ __forceinline__ int groups_among(int positions)
 {
-    int all = 0;
-    for (int e = threadIdx.x & 63; e < g.experts; e += 64) {
-        const int lo = min(max(g.offsets[e], 0), g.l.M), hi = min(max(g.offsets[e + 1], lo), g.l.M);
-        all += (hi - lo + ROWS - 1) / ROWS;
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
-    return __builtin_amdgcn_readfirstlane(all);
+    const int rest = positions % ROWS;
+    if (KIND == kRest) return rest > 0 && rest <= ROWS / 2;
+    return positions / ROWS + (KIND == kAll ? rest > 0 : rest > ROWS / 2);
 }
 
-// The `slot`-th group of ROWS positions (the last one of an expert may have fewer), expert by expert.  A wave asks, all of its lanes together; the answer is the same in
-// all.  Whatever the offsets hold, the positions returned are in [0, M).
-template <int ROWS>
-__device__ __forceinline__ Place place_of(const GroupedArgs &g, int slot)
-{
-    const int lane = threadIdx.x & 63;
-    Place p = {-1, 0, 0};
-    for (int base = 0; base < g.experts; base += 64) {
-        const int e = min(base + lane, g.experts - 1);
-        const int lo = min(max(g.offsets[e], 0), g.l.M), hi = min(max(g.offsets[e + 1], lo), g.l.M);
-        const int own = base + lane < g.experts ? (hi - lo + ROWS - 1) / ROWS : 0;
-        int up = own;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int below = __shfl_up(up, d);
-            if (lane >= d) up += below;
-        }
-        const unsigned long long beyond = __ballot(up > slot);
-        if (beyond) {
-            const int at = __builtin_ctzll(beyond);
-            const int before = __builtin_amdgcn_readlane(up - own, at);
-            const int first = __builtin_amdgcn_readlane(lo, at);
-            p.m0 = first + (slot - before) * ROWS;
-            p.end = __builtin_amdgcn_readlane(hi, at);
-            p.expert = p.m0 >= first && p.m0 < p.end ? base + at : -1;         // (always, but where sums of offsets that do not ascend have left 32 bits)
-            return p;
-        }
-        slot -= __builtin_amdgcn_readlane(up, 63);
+// The experts' positions as a wave asks for them, all of its lanes together: lane l has the first 64 experts' l-th, so that a second question does not wait for memory again.
+// The answers are the same in all lanes.  Whatever the offsets hold, the positions are in [0, M).
+struct Shares {
+    const GroupedArgs &g;
+    int lo0, hi0;
+
+    __device__ __forceinline__ explicit Shares(const GroupedArgs &args) : g(args) { load(0, &lo0, &hi0); }
+
+    __device__ __forceinline__ void load(int base, int *lo, int *hi) const
+    {
+        const int e = base + (int)(threadIdx.x & 63), at = min(e, g.experts - 1), a = g.offsets[at], b = g.offsets[at + 1];
+        *lo = min(max(a, 0), g.l.M);
+        *hi = e < g.experts ? min(max(b, *lo), g.l.M) : *lo;
     }
-    return p;
-}
+
+    // How many groups there are
+    template <int ROWS, Groups KIND>
+    __device__ __forceinline__ int groups() const
+    {
+        int all = groups_among<ROWS, KIND>(hi0 - lo0);
+        for (int base = 64; base < g.experts; base += 64) {
+            int lo, hi;
+            load(base, &lo, &hi);
+            all += groups_among<ROWS, KIND>(hi - lo);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
+        return __builtin_amdgcn_readfirstlane(all);
+    }
+
+    // The `slot`-th of them, expert by expert
+    template <int ROWS, Groups KIND = kAll>
+    __device__ __forceinline__ Place place(int slot) const
+    {
+        const int lane = threadIdx.x & 63;
+        Place p = {-1, 0, 0};
+        int lo = lo0, hi = hi0;
+        for (int base = 0;;) {
+            const int own = groups_among<ROWS, KIND>(hi - lo);
+            int up = own;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int below = __shfl_up(up, d);
+                if (lane >= d) up += below;
+            }
+            const unsigned long long beyond = __ballot(up > slot);
+            if (beyond) {
+                const int at = __builtin_ctzll(beyond);
+                const int before = __builtin_amdgcn_readlane(up - own, at), first = __builtin_amdgcn_readlane(lo, at);
+                p.end = __builtin_amdgcn_readlane(hi, at);
+                p.m0 = KIND == kRest ? first + (p.end - first) / ROWS * ROWS : first + (slot - before) * ROWS;
+                p.expert = p.m0 >= first && p.m0 < p.end ? base + at : -1;     // (always, but where sums of offsets that do not ascend have left 32 bits)
+                return p;
+            }
+            slot -= __builtin_amdgcn_readlane(up, 63);
+            base += 64;
+            if (base >= g.experts) return p;
+            load(base, &lo, &hi);
+        }
+    }
+};
 
 // x's row of position m: -1 where the index names none
 __device__ __forceinline__ int row_of(const GroupedArgs &g, int m)

@@ -14,7 +14,7 @@ __global__ __launch_bounds__(256) void grouped_plain_kernel(const GroupedArgs ga
 {
     const long long tile = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (tile >= tiles) return;
-    const Place p = place_of<16>(ga, __builtin_amdgcn_readfirstlane((int)(tile / tiles_n)));
+    const Place p = Shares(ga).place<16>(__builtin_amdgcn_readfirstlane((int)(tile / tiles_n)));
     if (p.expert < 0) return;
     const LinearArgs a = of_expert<GATED>(ga, p.expert, p.end);
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(256) void grouped_plain_kernel(const GroupedArgs ga
 template <int MT, bool GATED, bool DIRECT>
 __global__ __launch_bounds__(NW * 64) void grouped_few_kernel(const GroupedArgs ga, int tiles_n)
 {
-    const Place p = place_of<16 * MT>(ga, (int)blockIdx.x / tiles_n);
+    const Place p = Shares(ga).place<16 * MT>((int)blockIdx.x / tiles_n);
     if (p.expert < 0) return;
     few_product<MT, GATED, DIRECT, true>(of_expert<GATED>(ga, p.expert, p.end), &ga, (int)blockIdx.x % tiles_n * 16, p.m0);
 }
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(NW * 64) void grouped_few_kernel(const GroupedArgs 
 template <int C, int KW, int OUT, bool GATED>
 __global__ __launch_bounds__(64 * (KW > 4 ? KW : 4)) void grouped_tokens_kernel(const GroupedArgs ga, int blocks_n)
 {
-    const Place p = place_of<1>(ga, (int)blockIdx.x / blocks_n);
+    const Place p = Shares(ga).place<1>((int)blockIdx.x / blocks_n);
     if (p.expert < 0) return;
     const int row = __builtin_amdgcn_readfirstlane(row_of(ga, p.m0));
     if (row < 0) return;

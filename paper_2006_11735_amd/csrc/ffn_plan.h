@@ -230,9 +230,12 @@ inline bool grouped_tiled_takes(const GroupedArgs &a) { return a.l.K >= 16 && a.
 inline bool grouped_few_takes(const GroupedArgs &a) { return a.l.K >= 16 && a.l.ldw <= (1 << 26); }
 inline bool grouped_tokens_takes(const GroupedArgs &a) { return a.l.K >= 16 && a.l.K <= 32768 && a.l.M <= 64; }
 
+// (beside the sizes of kTiles: tiles of 256 x 256 and of 128 x 256 in one launch)
+constexpr int kMixedTiles = kTileKinds;
+
 struct GroupedPlan {
     LinearKernel kernel;
-    int tile;                      // of LinearKernel::tiled: its place in kTiles
+    int tile;                      // of LinearKernel::tiled: its place in kTiles, or kMixedTiles
     int rows;                      // of LinearKernel::few: positions a group, 16, 32 or 64
 };
 
@@ -242,33 +245,52 @@ inline GroupedPlan plan_grouped(const GroupedArgs &a, const LinearTuning &tuning
     const int force = tuning.kernel;
     const float positions = (float)a.l.M, experts = (float)a.experts, reached = experts * (1.f - __builtin_expf(-positions / experts)), share = positions / reached;
     GroupedPlan p = {LinearKernel::plain, 0, 16};
-    // (token by token an expert's weights are read for each of its positions)
-    if (grouped_tokens_takes(a) && (force == 2 || (force == 0 && share <= 1.3f))) {
+    // Position by position an expert's weights are read for each (8 positions of 8 experts, 1024 -> 2048: 4.8 us, by the kernel for few rows 5.8; 32 of 8: 8.8 and 6.7)
+    if (grouped_tokens_takes(a) && (force == 2 || (force == 0 && share <= 1.6f && a.l.M <= 16))) {
         p.kernel = LinearKernel::tokens;
         return p;
     }
+    // The kernel for few rows: a start, and a workgroup's own start and turns for each group and 16 outputs, more where groups are fuller, or a wave's turns one after the
+    // other; rows at odd places take twice as long (64 positions of 64 experts: 1024 -> 2048 17.2 us, 4096 -> 1024 16.7, 2001 -> 1501 27.5, gated 32, 32 and 46; 256 of 64: 25,
+    // 27 and 45; 32 of 8: 6.7, 9.1 and 11; 128 of 8: 12, 16 and 23)
     const bool few = grouped_few_takes(a), tiled = grouped_tiled_takes(a);
-    if (few && (force == 3 || (force == 0 && (!tiled || share <= 24.f)))) {
+    const float turns_few = (float)((a.l.K + kFewWaves * kFewTurn - 1) / (kFewWaves * kFewTurn)), groups_few = reached * (share / 16.f + 0.6f) * (float)((a.l.N + 15) / 16);
+    const float flow = (a.l.w2 ? 2.f : 1.f) * (step < 1.5f ? 1.f : 2.f) * (0.0024f + 0.0012f * turns_few) * groups_few, chain = turns_few * (share > 8.f ? 2.5f : 1.2f);
+    const float few_us = 4.f + (flow > chain ? flow : chain);
+    if (few && (force == 3 || (force == 0 && !tiled))) {
         p.kernel = LinearKernel::few;
         p.rows = share <= 16.f ? 16 : share <= 32.f ? 32 : 64;
         return p;
     }
     if (!tiled || (force != 0 && force < 4)) return p;
     p.kernel = LinearKernel::tiled;
-    if (force >= 10) { p.tile = force - 4; return p; }
+    // Of an expert's last group half is taken to be empty.  The way to a tile, by offsets and index, is 2.5 us more than that of a dense one.
     float best = 0.f;
-    const float steps = (float)((a.l.K + 127) / 128);
-    for (int c = 0; c < kTileKinds; ++c) {
-        const TileCost &t = kTiles[c];
+    const float steps = (float)((a.l.K + 127) / 128), weight_rows = (float)((a.l.w2 ? 2ll : 1ll) * a.l.N);
+    for (int c = 0; c <= kMixedTiles; ++c) {
         if (force >= 4 && c != force - 4) continue;
-        const float tiles = reached * __builtin_ceilf(share / (float)t.m) * (float)(((a.l.w2 ? 2ll : 1ll) * a.l.N + t.n - 1) / t.n);
-        const float turns = __builtin_ceilf(tiles / (float)t.held), on = tiles < (float)t.held ? tiles / 256.f : (float)t.held / 256.f;
-        const float full = t.held == 256 ? on : on < 1.f ? 0.25f * on : 0.25f + 0.75f * (on - 1.f);
-        const float us = turns * (t.fixed + steps * step * (t.few + (t.all - t.few) * full));
+        const TileCost &t = kTiles[c < kTileKinds ? c : 0];
+        const float tiles_n = __builtin_ceilf(weight_rows / (float)t.n);
+        float us;
+        if (c == kMixedTiles) {
+            const TileCost &half = kTiles[1];
+            const float big = t.fixed + steps * step * t.all, small = half.fixed + steps * step * half.all, all = reached * tiles_n * (share / (float)t.m * big + 0.5f * small) / 256.f;
+            us = (all > big ? all : big) + 0.4f * small;
+        } else {
+            const float groups = share / (float)t.m + 0.5f, tiles = reached * (groups > 1.f ? groups : 1.f) * tiles_n;
+            const float turns = __builtin_ceilf(tiles / (float)t.held), on = tiles < (float)t.held ? tiles / 256.f : (float)t.held / 256.f;
+            const float full = t.held == 256 ? on : step > 1.f ? (on > 1.f ? 1.f : 0.15f * on) : on < 1.f ? 0.25f * on : 0.25f + 0.75f * (on - 1.f);
+            us = turns * (t.fixed + steps * step * (t.few + (t.all - t.few) * full));
+        }
+        us += 2.5f;
         if (best == 0.f || us < best) {
             best = us;
             p.tile = c;
         }
+    }
+    if (few && force == 0 && few_us < best) {
+        p.kernel = LinearKernel::few;
+        p.rows = 16;
     }
     return p;
 }

@@ -11,7 +11,7 @@ namespace icnn {
 
 namespace {
 
-// Tokens that share one mask of 32 bits an expert; chunks of so many masks a workgroup, counted in 16 bits
+// Tokens that share one mask of 32 bits an expert; chunks of whole masks a workgroup, counted in 8 bits or 16
 constexpr int kMask = 32, kWantedChunks = 256, kMostChunk = 32768;
 
 long long chunk_of(long long rows)
@@ -19,6 +19,8 @@ long long chunk_of(long long rows)
     const long long per = ((rows + kWantedChunks - 1) / kWantedChunks + kMask - 1) / kMask * kMask;
     return per < kMostChunk ? per : kMostChunk;
 }
+
+int count_bytes(long long chunk) { return chunk < 256 ? 1 : 2; }
 
 // Logits as numbers that are ordered as they are, of which 0 is never chosen (minus infinity, places behind the last expert).  A 16-bit logit leaves room for its expert,
 // counted from above: the numbers of a row are all different then, and the largest of equal logits is the lowest expert's.
@@ -122,16 +124,20 @@ __device__ __forceinline__ int scan_counts(int *counts, int *first, int experts)
 }  // namespace
 
 // LANES lanes a token with P experts each, next to each other.  ONE: all rows are this workgroup's, which then places them too.
-template <int LANES, int P, int DT, bool ONE>
-__global__ __launch_bounds__(256) void route_choose_kernel(const RouteArgs a, int chunk)
+// As many threads as a mask's tokens want, at most 1024: by half of them, in two turns, 8192 x 256, top 8 took 8.6 us instead of 6.2; one wave for a few tokens
+template <int LANES>
+constexpr int kChooseThreads = kMask * LANES < 1024 ? kMask * LANES : 1024;
+
+template <int LANES, int P, int DT, int THREADS, bool ONE>
+__global__ __launch_bounds__(THREADS) void route_choose_kernel(const RouteArgs a, int chunk)
 {
-    constexpr int TOKENS = 256 / LANES;                    // at a time
+    constexpr int TOKENS = THREADS / LANES;                // at a time
     __shared__ uint32_t mask[kMostExperts];
     __shared__ int counts[kMostExperts], first[ONE ? kMostExperts : 1];
     const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES, e0 = lane * P;
     const long long begin = (long long)blockIdx.x * chunk;
     const int mine = (int)min((long long)chunk, a.rows - begin);
-    for (int e = threadIdx.x; e < a.experts; e += 256) {
+    for (int e = threadIdx.x; e < a.experts; e += THREADS) {
         mask[e] = 0;
         counts[e] = 0;
     }
@@ -208,7 +214,7 @@ __global__ __launch_bounds__(256) void route_choose_kernel(const RouteArgs a, in
         }
         if (!ONE) {
             __syncthreads();
-            for (int e = threadIdx.x; e < a.experts; e += 256) {
+            for (int e = threadIdx.x; e < a.experts; e += THREADS) {
                 counts[e] += __popc(mask[e]);
                 mask[e] = 0;
             }
@@ -217,13 +223,13 @@ __global__ __launch_bounds__(256) void route_choose_kernel(const RouteArgs a, in
     }
     if (ONE) {                                             // (one mask an expert holds all rows)
         __syncthreads();
-        for (int e = threadIdx.x; e < a.experts; e += 256) counts[e] = __popc(mask[e]);
+        for (int e = threadIdx.x; e < a.experts; e += THREADS) counts[e] = __popc(mask[e]);
         __syncthreads();
-        const int total = scan_counts<256>(counts, first, a.experts);
-        for (int e = threadIdx.x; e < a.experts; e += 256) a.offsets[e] = first[e];
+        const int total = scan_counts<THREADS>(counts, first, a.experts);
+        for (int e = threadIdx.x; e < a.experts; e += THREADS) a.offsets[e] = first[e];
         if (threadIdx.x == 0) a.offsets[a.experts] = total;
-        for (int i = total + threadIdx.x; i < mine * a.top; i += 256) a.token[i] = -1;
-        for (int i = threadIdx.x; i < mine * a.top; i += 256) {
+        for (int i = total + threadIdx.x; i < mine * a.top; i += THREADS) a.token[i] = -1;
+        for (int i = threadIdx.x; i < mine * a.top; i += THREADS) {
             const int t = i / a.top, e = a.expert[i];      // (this workgroup's own, written in front of a barrier)
             int p = -1;
             if (e >= 0) {
@@ -233,73 +239,142 @@ __global__ __launch_bounds__(256) void route_choose_kernel(const RouteArgs a, in
             a.place[i] = p;
         }
     } else {
-        for (int e = threadIdx.x; e < a.experts; e += 256) a.counts[(long long)blockIdx.x * ((a.experts + 7) / 8 * 8) + e] = (uint16_t)counts[e];
+        for (int e = threadIdx.x; e < a.experts; e += THREADS) {
+            if (chunk < 256) ((uint8_t *)a.counts)[(long long)blockIdx.x * ((a.experts + 15) / 16 * 16) + e] = (uint8_t)counts[e];
+            else ((uint16_t *)a.counts)[(long long)blockIdx.x * ((a.experts + 7) / 8 * 8) + e] = (uint16_t)counts[e];
+        }
     }
 }
 
-// The places of a chunk's choices, from all chunks' counts.
-__global__ __launch_bounds__(1024) void route_place_kernel(const RouteArgs a, int chunk)
+// The places of a chunk's choices, from all chunks' counts, of BYTES each.
+constexpr int kPlaceThreads = 512;
+
+template <int BYTES>
+__global__ __launch_bounds__(kPlaceThreads) void route_place_kernel(const RouteArgs a, int chunk)
 {
+    constexpr int THREADS = kPlaceThreads, EACH = 16 / BYTES, CHOICES = kMask * kMostTop / THREADS;
     __shared__ uint32_t mask[kMostExperts];
-    __shared__ int total[kMostExperts], before[kMostExperts], first[kMostExperts];
+    __shared__ int total[kMostExperts], before[kMostExperts], first[kMostExperts];         // expert EACH p + e's at e * pieces + p: lanes that add meet no bank twice
     const int chunks = gridDim.x, t = threadIdx.x;
     const long long begin = (long long)blockIdx.x * chunk;
-    const int mine = (int)min((long long)chunk, a.rows - begin);
-    for (int e = t; e < a.experts; e += 1024) {
-        mask[e] = 0;
-        total[e] = before[e] = 0;
-    }
+    const int mine = (int)min((long long)chunk, a.rows - begin), pieces = (a.experts + EACH - 1) / EACH;
+    auto slot_of = [&](int e) { return e % EACH * pieces + e / EACH; };
+    // (a mask's choices, on their way early)
+    int chosen[CHOICES];
+    auto fetch = [&](int base) {
+#pragma unroll
+        for (int i = 0; i < CHOICES; ++i) {
+            const int c = i * THREADS + t;
+            chosen[i] = c < min(kMask, mine - base) * a.top ? a.expert[(begin + base) * a.top + c] : -1;
+        }
+    };
+    fetch(0);
+    for (int e = t; e < kMostExperts; e += THREADS) mask[e] = total[e] = before[e] = 0;
     __syncthreads();
-    // Eight experts a thread, of every so many-th chunk: a chunk's counts are in whole 16 bytes (256 chunks of 256 experts: eight loads a thread, one by one 64)
-    const int pieces = (a.experts + 7) / 8, ways = 1024 / pieces, piece = t % pieces, way = t / pieces;
+    // A thread has 16 bytes of counts of every so many-th chunk
+    const int ways = THREADS / pieces, piece = t % pieces, way = t / pieces;
     if (way < ways) {
-        int all[8] = {}, low[8] = {};
+        int all[EACH] = {}, low[EACH] = {};
+        // (bytes are added two to a register, 16 bits each: no more than 256 chunks of less than 256 rows have counts of a byte)
+        uint32_t all2[8] = {}, low2[8] = {};
 #pragma unroll 4
         for (int q = way; q < chunks; q += ways) {
             const v4i v = *((const v4i *)a.counts + (long long)q * pieces + piece);
+            const uint32_t lower = q < (int)blockIdx.x ? ~0u : 0u;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int n = (int)((uint32_t)v[e >> 1] >> (16 * (e & 1)) & 0xffffu);
-                all[e] += n;
-                low[e] += q < (int)blockIdx.x ? n : 0;
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (BYTES == 1) {
+                    const uint32_t even = (uint32_t)v[i] & 0xff00ffu, odd = (uint32_t)v[i] >> 8 & 0xff00ffu;
+                    all2[2 * i] += even;
+                    all2[2 * i + 1] += odd;
+                    low2[2 * i] += even & lower;
+                    low2[2 * i + 1] += odd & lower;
+                } else {
+                    const int n0 = v[i] & 0xffff, n1 = (int)((uint32_t)v[i] >> 16);
+                    all[2 * i] += n0;
+                    all[2 * i + 1] += n1;
+                    low[2 * i] += n0 & (int)lower;
+                    low[2 * i + 1] += n1 & (int)lower;
+                }
+            }
+        }
+        if constexpr (BYTES == 1) {
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                all[e] = (int)(all2[(e >> 2) * 2 + (e & 1)] >> (8 * (e & 2)) & 0xffffu);
+                low[e] = (int)(low2[(e >> 2) * 2 + (e & 1)] >> (8 * (e & 2)) & 0xffffu);
             }
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (8 * piece + e < a.experts) {
-                atomicAdd(&total[8 * piece + e], all[e]);
-                atomicAdd(&before[8 * piece + e], low[e]);
-            }
+        for (int e = 0; e < EACH; ++e) {
+            atomicAdd(&total[e * pieces + piece], all[e]);
+            atomicAdd(&before[e * pieces + piece], low[e]);
+        }
     }
     __syncthreads();
-    const int sum = scan_counts<1024>(total, first, a.experts);
-    if (blockIdx.x == 0) {
-        for (int e = t; e < a.experts; e += 1024) a.offsets[e] = first[e];
-        if (t == 0) a.offsets[a.experts] = sum;
-    }
-    for (long long i = sum + (long long)blockIdx.x * 1024 + t; i < a.rows * a.top; i += (long long)chunks * 1024) a.token[i] = -1;
-    if (t < a.experts) first[t] += before[t];
-    __syncthreads();
-    for (int base = 0; base < mine; base += kMask) {
-        const int many = min(kMask, mine - base) * a.top;  // (at most 512)
-        const long long at = (begin + base) * a.top;
-        const int e = t < many ? a.expert[at + t] : -1, row = t / a.top;
-        if (e >= 0) atomicOr(&mask[e], 1u << row);
+    int sum = 0;
+    {                                                      // first[e]: the places of lower experts, and of this one's in front of the chunk
+        constexpr int PER = kMostExperts / THREADS;
+        __shared__ int sums[THREADS / 64];
+        int own = 0, count[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            count[i] = t * PER + i < a.experts ? total[slot_of(t * PER + i)] : 0;
+            own += count[i];
+        }
+        int up = own;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int below = __shfl_up(up, d);
+            if ((t & 63) >= d) up += below;
+        }
+        if ((t & 63) == 63) sums[t >> 6] = up;
         __syncthreads();
-        if (t < many) {
+        int at = up - own;
+#pragma unroll
+        for (int q = 0; q < THREADS / 64; ++q) {
+            if (q < t >> 6) at += sums[q];
+            sum += sums[q];
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = t * PER + i;
+            if (e < a.experts) {
+                first[e] = at + before[slot_of(e)];
+                if (blockIdx.x == 0) a.offsets[e] = at;
+            }
+            at += count[i];
+        }
+        if (blockIdx.x == 0 && t == 0) a.offsets[a.experts] = sum;
+    }
+    for (long long i = sum + (long long)blockIdx.x * THREADS + t; i < a.rows * a.top; i += (long long)chunks * THREADS) a.token[i] = -1;
+    for (int base = 0; base < mine; base += kMask) {
+        const int many = min(kMask, mine - base) * a.top;
+        const long long at = (begin + base) * a.top;
+        if (base) fetch(base);
+#pragma unroll
+        for (int i = 0; i < CHOICES; ++i)
+            if (chosen[i] >= 0) atomicOr(&mask[chosen[i]], 1u << ((i * THREADS + t) / a.top));
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < CHOICES; ++i) {
+            const int c = i * THREADS + t, row = c / a.top;
+            if (c >= many) continue;
             int p = -1;
-            if (e >= 0) {
-                p = first[e] + __popc(mask[e] & ((1u << row) - 1));
+            if (chosen[i] >= 0) {
+                p = first[chosen[i]] + __popc(mask[chosen[i]] & ((1u << row) - 1));
                 a.token[p] = (int)(begin + base + row);
             }
-            a.place[at + t] = p;
+            a.place[at + c] = p;
         }
-        __syncthreads();
-        if (t < a.experts) {
-            first[t] += __popc(mask[t]);
-            mask[t] = 0;
+        if (base + kMask < mine) {
+            __syncthreads();
+            for (int e = t; e < a.experts; e += THREADS) {
+                first[e] += __popc(mask[e]);
+                mask[e] = 0;
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
@@ -307,21 +382,27 @@ size_t route_workspace(long long rows, int experts)
 {
     if (rows <= kMask) return 0;
     const long long chunk = chunk_of(rows);
-    return (size_t)((rows + chunk - 1) / chunk) * (size_t)((experts + 7) / 8) * 16;
+    return (size_t)((rows + chunk - 1) / chunk) * (size_t)((experts * count_bytes(chunk) + 15) / 16) * 16;
 }
 
 template <int LANES, int P, int DT>
 static hipError_t launch_of(const RouteArgs &a, hipStream_t st)
 {
+    constexpr int MANY = kChooseThreads<LANES>;
+    if (a.rows <= 64 / LANES) {
+        hipLaunchKernelGGL((route_choose_kernel<LANES, P, DT, 64, true>), dim3(1), dim3(64), 0, st, a, kMask);
+        return hipGetLastError();
+    }
     if (a.rows <= kMask) {
-        hipLaunchKernelGGL((route_choose_kernel<LANES, P, DT, true>), dim3(1), dim3(256), 0, st, a, kMask);
+        hipLaunchKernelGGL((route_choose_kernel<LANES, P, DT, MANY, true>), dim3(1), dim3(MANY), 0, st, a, kMask);
         return hipGetLastError();
     }
     const long long chunk = chunk_of(a.rows);
     const unsigned chunks = (unsigned)((a.rows + chunk - 1) / chunk);
-    hipLaunchKernelGGL((route_choose_kernel<LANES, P, DT, false>), dim3(chunks), dim3(256), 0, st, a, (int)chunk);
+    hipLaunchKernelGGL((route_choose_kernel<LANES, P, DT, MANY, false>), dim3(chunks), dim3(MANY), 0, st, a, (int)chunk);
     if (hipError_t e = hipGetLastError()) return e;
-    hipLaunchKernelGGL(route_place_kernel, dim3(chunks), dim3(1024), 0, st, a, (int)chunk);
+    if (count_bytes(chunk) == 1) hipLaunchKernelGGL(route_place_kernel<1>, dim3(chunks), dim3(kPlaceThreads), 0, st, a, (int)chunk);
+    else hipLaunchKernelGGL(route_place_kernel<2>, dim3(chunks), dim3(kPlaceThreads), 0, st, a, (int)chunk);
     return hipGetLastError();
 }
 

@@ -71,9 +71,19 @@ __device__ __forceinline__ void drain(v16i (&acc)[TN][TM])
 
 }  // namespace
 
-// GROUPED: tiles of the experts' groups of positions (see ffn_grouped.hip), whose number only the device knows; k is whole
+// Tile `slot` of tiles_m x tiles_n: eight rows of tiles, column after column, so that what an XCD has at one time shares its weights and rows
+__device__ __forceinline__ void tile_at(int slot, int tiles_m, int tiles_n, int *tm, int *tn)
+{
+    constexpr int GROUP = 8;
+    const int panel = slot / (GROUP * tiles_n), in_panel = slot - panel * GROUP * tiles_n, high = min(GROUP, tiles_m - panel * GROUP);
+    *tn = in_panel / high;
+    *tm = panel * GROUP + in_panel - *tn * high;
+}
+
+// A tile: rows m0 .. of `a` (its M is where they end) and outputs n0 ...  Of a k axis in ranges (ta.splits) this is range `range` of tile `slot`, unit `unit` of all.
+// GROUPED: rows of an expert (see ffn_grouped.hip), x's being what the index says; k is whole.
 template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED, bool DIRECT, bool GROUPED>
-__device__ __forceinline__ void tiled_product(const TiledArgs &ta, const GroupedArgs *ga)
+__device__ __forceinline__ void tiled_product(const TiledArgs &ta, const LinearArgs &a, const GroupedArgs *ga, int n0, int m0, int unit, int slot, int range)
 {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-resource type exists in the device pass only
     constexpr int NW = WN * WM, BN = 32 * TN * WN, BM = 32 * TM * WM, ROWS = 1024 / BK, PIECES = BK / 16, SLICES = BK / 32;
@@ -81,21 +91,7 @@ __device__ __forceinline__ void tiled_product(const TiledArgs &ta, const Grouped
     static_assert(DIRECT || STAGES == 2, "copies through registers are one stage ahead");
     static_assert(LW * ROWS * NW == BN && LX * ROWS * NW == BM && SLICES >= 2 && SLICES % 2 == 0, "whole copies, two fragment sets in turn");
     extern __shared__ __align__(1024) uint8_t lds[];
-    const int tiles_m = GROUPED ? min(groups_of<BM>(*ga), ta.tiles_m) : ta.tiles_m, splits = GROUPED ? 1 : ta.splits, per_xcd = GROUPED ? (tiles_m * ta.tiles_n + 7) / 8 : ta.per_xcd;
-    if (GROUPED && (int)(blockIdx.x >> 3) >= per_xcd) return;
-    const int unit = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-    if (unit >= ta.tiles_n * tiles_m * splits) return;
-    const int slot = unit / splits, range = unit - slot * splits;
-    // eight rows of tiles, column after column: what an XCD has at one time shares its weights and rows
-    constexpr int GROUP = 8;
-    const int panel = slot / (GROUP * ta.tiles_n), in_panel = slot - panel * GROUP * ta.tiles_n, high = min(GROUP, tiles_m - panel * GROUP);
-    const int tn0 = in_panel / high, tm0 = panel * GROUP + in_panel - tn0 * high;
-    const Place place = GROUPED ? place_of<BM>(*ga, tm0) : Place{0, tm0 * BM, ta.l.M};
-    if (GROUPED && place.expert < 0) return;
-    const LinearArgs a = GROUPED ? of_expert<GATED>(*ga, place.expert, place.end) : ta.l;
-    const int n0 = tn0 * (GATED ? BN / 2 : BN), m0 = place.m0;
     const bool indexed = GROUPED && ga->index;
-
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wave % WN, wm = wave / WN;
 

@@ -211,7 +211,7 @@ def kernel():
 
 
 @pytest.mark.parametrize("which,counts", [(1, [3, 0, 40]), (2, [1, 0, 2, 5]), (2, [20, 3, 0, 17]), (3, [1, 0, 30]), (3, [64, 0, 65, 17])] +
-                         [(k, c) for k in range(4, 10) for c in ([1, 0, 2], [63, 64, 0, 65], [300, 5, 130])])
+                         [(k, c) for k in range(4, 11) for c in ([1, 0, 2], [63, 64, 0, 65], [300, 5, 130])] + [(10, [128, 129, 0, 256]), (10, [384, 1, 257, 700, 0, 60])])
 @pytest.mark.parametrize("k,n", [(16, 16), (64, 7), (300, 96), (512, 260), (1040, 129), (2320, 520)])
 def test_every_kernel(kernel, which, counts, k, n):
     kernel(which)

@@ -65,7 +65,7 @@ def test_experts(experts, rows):
         Router(logits_of(rows, experts, experts + top), top, "f16", "sigmoid", top % 2 == 1, 2.5).go()
 
 
-@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 500, 1000, 4097, 8192, 8193, 20011])
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 500, 1000, 4097, 8192, 8193, 20011, 70001])
 @pytest.mark.parametrize("experts,top", [(8, 2), (64, 6), (256, 8)])
 def test_rows(rows, experts, top):
     Router(logits_of(rows, experts, rows), top, "bf16", "softmax", True).go()
