@@ -193,3 +193,18 @@ def test_lists_of_calls_refuse_as_the_calls_do():
                ("grouped_gated_linear", (B.grouped_desc(rows=0, k=64, n=32, experts=4), *[None] * 11)), ("linear_s4", (B.linear_s4_desc(rows=0, k=64, n=32), *[None] * 7)),
                ("gated_linear_s4", (B.linear_s4_desc(rows=0, k=64, n=32), *[None] * 9))]
     B.Calls(nothing).run(stream=0)
+
+
+def test_blocks_refuse_shapes_that_do_not_fit():
+    import torch
+    from paper_2006_11735_amd.ffn import ExpertsFeedForward, FeedForward
+    z = torch.zeros
+    good = dict(gamma=z(8), w_router=z(4, 8), w_gate=z(4, 16, 8), w_up=z(4, 16, 8), w_down=z(4, 8, 16), rows=4, top=2)
+    for kw in (dict(gamma=z(9)), dict(w_router=z(8, 4)), dict(w_gate=z(16, 8)), dict(w_up=z(4, 16, 9)), dict(w_down=z(4, 16, 8)), dict(b_router=z(5)), dict(b_gate=z(4, 8)),
+               dict(b_down=z(8)), dict(w_up=None, b_up=z(4, 16)), dict(act="tanh"), dict(dtype=torch.float64), dict(rows=0), dict(top=0), dict(top=5), dict(score="linear")):
+        with pytest.raises(ValueError):
+            ExpertsFeedForward(**{**good, **kw})
+    good = dict(gamma=z(8), w_gate=z(16, 8), w_up=z(16, 8), w_down=z(8, 16), rows=4)
+    for kw in (dict(bits=2), dict(bits=4, group=48), dict(bits=4, scale_dtype=torch.int8)):
+        with pytest.raises(ValueError):
+            FeedForward(**{**good, **kw})
