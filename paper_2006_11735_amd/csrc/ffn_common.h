@@ -183,6 +183,16 @@ __device__ __forceinline__ Eight<DT> load_eight(const void *p, long long i)
     return r;
 }
 
+// The same of what is read once and not to be kept
+template <int DT>
+__device__ __forceinline__ Eight<DT> load_eight_once(const void *p, long long i)
+{
+    Eight<DT> r;
+#pragma unroll
+    for (int q = 0; q < (DT == kF32 ? 2 : 1); ++q) r.b[q] = __builtin_nontemporal_load((const v4i_any *)((const uint8_t *)p + i * (DT == kF32 ? 4 : 2)) + q);
+    return r;
+}
+
 template <int DT>
 __device__ __forceinline__ float value_of(const Eight<DT> &r, int e)
 {

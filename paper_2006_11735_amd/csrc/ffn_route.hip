@@ -85,39 +85,39 @@ __device__ __forceinline__ float sum_over(float v)
     return __builtin_bit_cast(float, over_lanes<LANES>(__builtin_bit_cast(uint32_t, v), Sum{}));
 }
 
-// Exclusive sums of `experts` counts in LDS, by all threads of the workgroup; the total is returned
-template <int THREADS>
-__device__ __forceinline__ int scan_counts(int *counts, int *first, int experts)
+// first[e] = the sum of count(0 .. e - 1), by all threads of the workgroup; the total is returned
+template <int THREADS, class F>
+__device__ __forceinline__ int scan_counts(int experts, int *first, F &&count)
 {
-    constexpr int PER = kMostExperts / THREADS < 1 ? 1 : kMostExperts / THREADS, WAVES = THREADS / 64;
+    constexpr int WAVES = THREADS / 64;
     __shared__ int sums[WAVES];
     const int t = threadIdx.x, lane = t & 63;
-    int mine[PER], own = 0;
+    int total = 0;
+    for (int base = 0; base < experts; base += THREADS) {
+        const int own = base + t < experts ? count(base + t) : 0;
+        int up = own;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        mine[i] = t * PER + i < experts ? counts[t * PER + i] : 0;
-        own += mine[i];
-    }
-    int up = own;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int below = __shfl_up(up, d);
+            if (lane >= d) up += below;
+        }
+        if (WAVES > 1) {
+            if (base) __syncthreads();                     // (the sums of the turn before have been read)
+            if (lane == 63) sums[t >> 6] = up;
+            __syncthreads();
+        }
+        int before = total + up - own;
+        if (WAVES > 1) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int below = __shfl_up(up, d);
-        if (lane >= d) up += below;
+            for (int q = 0; q < WAVES; ++q) {
+                if (q < t >> 6) before += sums[q];
+                total += sums[q];
+            }
+        } else {
+            total += __builtin_amdgcn_readlane(up, 63);
+        }
+        if (base + t < experts) first[base + t] = before;
     }
-    if (lane == 63) sums[t >> 6] = up;
-    __syncthreads();
-    int before = up - own, total = 0;
-#pragma unroll
-    for (int q = 0; q < WAVES; ++q) {
-        if (q < t >> 6) before += sums[q];
-        total += sums[q];
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        if (t * PER + i < experts) first[t * PER + i] = before;
-        before += mine[i];
-    }
-    __syncthreads();
     return total;
 }
 
@@ -223,9 +223,8 @@ __global__ __launch_bounds__(THREADS) void route_choose_kernel(const RouteArgs a
     }
     if (ONE) {                                             // (one mask an expert holds all rows)
         __syncthreads();
-        for (int e = threadIdx.x; e < a.experts; e += THREADS) counts[e] = __popc(mask[e]);
+        const int total = scan_counts<THREADS>(a.experts, first, [&](int e) { return __popc(mask[e]); });
         __syncthreads();
-        const int total = scan_counts<THREADS>(counts, first, a.experts);
         for (int e = threadIdx.x; e < a.experts; e += THREADS) a.offsets[e] = first[e];
         if (threadIdx.x == 0) a.offsets[a.experts] = total;
         for (int i = total + threadIdx.x; i < mine * a.top; i += THREADS) a.token[i] = -1;
@@ -312,41 +311,13 @@ __global__ __launch_bounds__(kPlaceThreads) void route_place_kernel(const RouteA
         }
     }
     __syncthreads();
-    int sum = 0;
-    {                                                      // first[e]: the places of lower experts, and of this one's in front of the chunk
-        constexpr int PER = kMostExperts / THREADS;
-        __shared__ int sums[THREADS / 64];
-        int own = 0, count[PER];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            count[i] = t * PER + i < a.experts ? total[slot_of(t * PER + i)] : 0;
-            own += count[i];
-        }
-        int up = own;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int below = __shfl_up(up, d);
-            if ((t & 63) >= d) up += below;
-        }
-        if ((t & 63) == 63) sums[t >> 6] = up;
-        __syncthreads();
-        int at = up - own;
-#pragma unroll
-        for (int q = 0; q < THREADS / 64; ++q) {
-            if (q < t >> 6) at += sums[q];
-            sum += sums[q];
-        }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = t * PER + i;
-            if (e < a.experts) {
-                first[e] = at + before[slot_of(e)];
-                if (blockIdx.x == 0) a.offsets[e] = at;
-            }
-            at += count[i];
-        }
-        if (blockIdx.x == 0 && t == 0) a.offsets[a.experts] = sum;
+    // first[e]: the places of lower experts, and of this one's in front of the chunk
+    const int sum = scan_counts<THREADS>(a.experts, first, [&](int e) { return total[slot_of(e)]; });
+    for (int e = t; e < a.experts; e += THREADS) {         // (each thread its own)
+        if (blockIdx.x == 0) a.offsets[e] = first[e];
+        first[e] += before[slot_of(e)];
     }
+    if (blockIdx.x == 0 && t == 0) a.offsets[a.experts] = sum;
     for (long long i = sum + (long long)blockIdx.x * THREADS + t; i < a.rows * a.top; i += (long long)chunks * THREADS) a.token[i] = -1;
     for (int base = 0; base < mine; base += kMask) {
         const int many = min(kMask, mine - base) * a.top;
