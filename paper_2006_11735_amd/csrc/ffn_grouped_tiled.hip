@@ -15,7 +15,7 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
     tile_at(unit, tiles_m, ta.tiles_n, &tm, &tn);
     const Place p = shares.place<BM>(tm);
     if (p.expert < 0) return;
-    tiled_product<TN, TM, WN, WM, BK, STAGES, GATED, DIRECT, true>(ta, of_expert<GATED>(ga, p.expert, p.end), &ga, tn * (32 * TN * WN / (GATED ? 2 : 1)), p.m0, 0, 0, 0);
+    tiled_product<TN, TM, WN, WM, BK, STAGES, GATED, DIRECT, true>(ta, of_expert<GATED>(ga, p.expert, p.end), &ga, tn * (32 * TN * WN / (GATED ? 2 : 1)), p.m0);
 }
 
 template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED, bool DIRECT>
@@ -78,8 +78,8 @@ __global__ __launch_bounds__(512, 2) void grouped_mixed_kernel(const TiledArgs t
     }
     if (p.expert < 0 || p.m0 >= p.end) return;
     const LinearArgs a = of_expert<GATED>(ga, p.expert, p.end);
-    if (big) tiled_product<2, 4, 4, 2, 128, 2, GATED, DIRECT, true>(ta, a, &ga, tn * BN, p.m0, 0, 0, 0);
-    else tiled_product<2, 2, 4, 2, 128, DIRECT ? 3 : 2, GATED, DIRECT, true>(ta, a, &ga, tn * BN, p.m0, 0, 0, 0);
+    if (big) tiled_product<2, 4, 4, 2, 128, 2, GATED, DIRECT, true>(ta, a, &ga, tn * BN, p.m0);
+    else tiled_product<2, 2, 4, 2, 128, DIRECT ? 3 : 2, GATED, DIRECT, true>(ta, a, &ga, tn * BN, p.m0);
 }
 
 template <bool GATED, bool DIRECT>

@@ -245,6 +245,7 @@ __global__ __launch_bounds__(WN * WM * WK * 64, 2) void s4_tiled_kernel(const Li
     for (int s = 0; s < STAGES - 1; ++s) copy(s);
     for (int i = t; i < BM; i += S::THREADS) row_scales[i] = a.xs[min(m0 + i, a.M - 1)];
     if (S::AHEAD) {
+        asm volatile("" ::: "memory");
         FFN_WAIT_VMCNT((STAGES - 2) * COPIES);
         barrier();
         load_first(0);
@@ -252,6 +253,7 @@ __global__ __launch_bounds__(WN * WM * WK * 64, 2) void s4_tiled_kernel(const Li
 #pragma unroll 1
     for (int s = 0; s < steps; ++s) {
         const int c = s / STEPS, part = s % STEPS;
+        asm volatile("" ::: "memory");
         FFN_WAIT_VMCNT((S::AHEAD ? STAGES - 3 : STAGES - 2) * COPIES);     // (later ones are still in flight; others that are make this wait for more)
         barrier();
         if (part == 0) fetch_scales(c + 1);

@@ -80,10 +80,10 @@ __device__ __forceinline__ void tile_at(int slot, int tiles_m, int tiles_n, int 
     *tm = panel * GROUP + in_panel - *tn * high;
 }
 
-// A tile: rows m0 .. of `a` (its M is where they end) and outputs n0 ...  Of a k axis in ranges (ta.splits) this is range `range` of tile `slot`, unit `unit` of all.
-// GROUPED: rows of an expert (see ffn_grouped.hip), x's being what the index says; k is whole.
+// A tile: the workgroup's of all tiles of `a`, and of their k axis's ranges.  GROUPED: rows m0_of .. of an expert's (a.M is where they end; see ffn_grouped.hip), x's being
+// what the index says, and outputs n0_of ..; k is whole.
 template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED, bool DIRECT, bool GROUPED>
-__device__ __forceinline__ void tiled_product(const TiledArgs &ta, const LinearArgs &a, const GroupedArgs *ga, int n0, int m0, int unit, int slot, int range)
+__device__ __forceinline__ void tiled_product(const TiledArgs &ta, const LinearArgs &a, const GroupedArgs *ga, int n0_of, int m0_of)
 {
 #if defined(__HIP_DEVICE_COMPILE__)   // the buffer-resource type exists in the device pass only
     constexpr int NW = WN * WM, BN = 32 * TN * WN, BM = 32 * TM * WM, ROWS = 1024 / BK, PIECES = BK / 16, SLICES = BK / 32;
@@ -91,6 +91,12 @@ __device__ __forceinline__ void tiled_product(const TiledArgs &ta, const LinearA
     static_assert(DIRECT || STAGES == 2, "copies through registers are one stage ahead");
     static_assert(LW * ROWS * NW == BN && LX * ROWS * NW == BM && SLICES >= 2 && SLICES % 2 == 0, "whole copies, two fragment sets in turn");
     extern __shared__ __align__(1024) uint8_t lds[];
+    const int unit = GROUPED ? 0 : (int)(blockIdx.x & 7) * ta.per_xcd + (int)(blockIdx.x >> 3);
+    if (!GROUPED && unit >= ta.tiles_n * ta.tiles_m * ta.splits) return;
+    const int slot = GROUPED ? 0 : unit / ta.splits, range = GROUPED ? 0 : unit - slot * ta.splits;
+    int tm = 0, tn = 0;
+    if (!GROUPED) tile_at(slot, ta.tiles_m, ta.tiles_n, &tm, &tn);
+    const int n0 = GROUPED ? n0_of : tn * (GATED ? BN / 2 : BN), m0 = GROUPED ? m0_of : tm * BM;
     const bool indexed = GROUPED && ga->index;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wave % WN, wm = wave / WN;

@@ -6,12 +6,7 @@ namespace icnn {
 template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED, bool DIRECT>
 __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN + TM * WM) * BK * STAGES)) void linear_tiled_kernel(const TiledArgs ta)
 {
-    const int unit = (int)(blockIdx.x & 7) * ta.per_xcd + (int)(blockIdx.x >> 3);
-    if (unit >= ta.tiles_n * ta.tiles_m * ta.splits) return;
-    const int slot = unit / ta.splits;
-    int tm, tn;
-    tile_at(slot, ta.tiles_m, ta.tiles_n, &tm, &tn);
-    tiled_product<TN, TM, WN, WM, BK, STAGES, GATED, DIRECT, false>(ta, ta.l, nullptr, tn * (32 * TN * WN / (GATED ? 2 : 1)), tm * (32 * TM * WM), unit, slot, unit - slot * ta.splits);
+    tiled_product<TN, TM, WN, WM, BK, STAGES, GATED, DIRECT, false>(ta, ta.l, nullptr, 0, 0);
 }
 
 template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED, bool DIRECT>
