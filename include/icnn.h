@@ -127,7 +127,8 @@ int icnn_version(void);
 const char *icnn_last_error(void);
 
 /* Kernel-selection override, for sweeps and for tests that must reach a kernel the library would not pick
- * for a small shape.  It changes which kernel computes a layer, never a result.  Process-wide, not
+ * for a small shape.  It changes which kernel computes a layer, never a result (but for the last bits of
+ * products with 4-bit weights, whose groups are added in float32).  Process-wide, not
  * synchronised: set it while no other thread is inside the library.  `name` (host string) and the values it takes:
  *   "tile"        -1 library's choice; 0..4 force that tile shape of the tap-by-tap convolution kernel
  *   "stages"      0 library's choice; 2..6 LDS ring depth of that kernel
@@ -150,7 +151,9 @@ const char *icnn_last_error(void);
  *   "flat"        0 library's choice; 1 / 2: every / no layer whose shape it takes on the kernel that streams weights into registers
  *   "tri_tile"    0 library's choice; 1..4 = the 3x3 + 1x1 + 1x1 kernel at any size, in tiles of 32, 64, 96 or 112 pixels
  *   "ff_kernel"   0 library's choice; products of 8-bit rows, where the shape allows it, by 1 the plain kernel, 2 the one for up to four rows, 3 the one for up to 64
- *                 rows, 4..9 in tiles of 256 x 256, 128 x 256, 128 x 128 (two or one on a compute unit), 64 x 128, 64 x 64 rows x weight rows
+ *                 rows, 4..9 in tiles of 256 x 256, 128 x 256, 128 x 128 (two or one on a compute unit), 64 x 128, 64 x 64 rows x weight rows; those grouped by
+ *                 expert so too, 2 position by position (up to 64), 10 in tiles of 256 x 256 and 128 x 256; those with 4-bit weights by 1, 2 and, up to 32
+ *                 rows, 3 likewise, 4..6 in tiles of 128 x 256, 128 x 128, 64 x 32
  *   "ff_split"    0 library's choice; 1 their k axis stays whole; 2..16 it is split into up to so many ranges where the shape and the workspace allow
  *   "ksplit"      0, 1 never split the K axis over workgroups (the library's choice); 2..8 that split where it divides the K steps
  *   "reset"       (value ignored) back to the library's choices

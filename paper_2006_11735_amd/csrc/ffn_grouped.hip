@@ -35,6 +35,15 @@ __global__ __launch_bounds__(256) void grouped_plain_kernel(const GroupedArgs ga
     finish_four<GATED>(a, acc[0], acc[1], f, m, n0 + 4 * g);
 }
 
+static hipError_t launch_plain(const GroupedArgs &a, hipStream_t st)
+{
+    const int tiles_n = (a.l.N + 15) / 16;
+    const long long tiles = grouped_slots(a.l.M, a.experts, 16) * tiles_n, blocks = (tiles + 3) / 4;
+    if (a.l.w2) hipLaunchKernelGGL(grouped_plain_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, a, tiles_n, tiles);
+    else hipLaunchKernelGGL(grouped_plain_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, a, tiles_n, tiles);
+    return hipGetLastError();
+}
+
 template <int MT, bool GATED, bool DIRECT>
 __global__ __launch_bounds__(NW * 64) void grouped_few_kernel(const GroupedArgs ga, int tiles_n)
 {
@@ -63,7 +72,7 @@ static hipError_t launch_few_of(const GroupedArgs &a, hipStream_t st)
 {
     const int tiles_n = (a.l.N + 15) / 16;
     const long long groups = grouped_slots(a.l.M, a.experts, 16 * MT) * tiles_n;
-    if (!fits_launch(groups, NW * 64)) return hipErrorInvalidValue;
+    if (!fits_launch(groups, NW * 64)) return launch_plain(a, st);             // (which has four groups of 16 x 16 outputs in a workgroup)
     hipLaunchKernelGGL((grouped_few_kernel<MT, GATED, DIRECT>), dim3((unsigned)groups), dim3(NW * 64), (few_lds<MT, GATED>()), st, a, tiles_n);
     return hipGetLastError();
 }
@@ -102,11 +111,7 @@ hipError_t launch_grouped(const GroupedArgs &a, hipStream_t st)
     case LinearKernel::tiled: return launch_grouped_tiled(a, plan.tile, st);
     case LinearKernel::plain: break;
     }
-    const int tiles_n = (a.l.N + 15) / 16;
-    const long long tiles = grouped_slots(a.l.M, a.experts, 16) * tiles_n, blocks = (tiles + 3) / 4;
-    if (a.l.w2) hipLaunchKernelGGL(grouped_plain_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, a, tiles_n, tiles);
-    else hipLaunchKernelGGL(grouped_plain_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, a, tiles_n, tiles);
-    return hipGetLastError();
+    return launch_plain(a, st);
 }
 
 }  // namespace icnn
