@@ -315,13 +315,13 @@ struct LinearS4Args {
 };
 
 // Tiles of a product with 4-bit weights, one on a compute unit at a time: {rows, weight rows, us that do not depend on k, us for 128 numbers of k in groups of 32, of 64 and of
-// 128 or 256}.  Measured with 8192 -> 8192: 1024 rows by the first 84 us (by the second 98), 512 by the second 50 (84), 64 by the third 19 (46); in groups of 32 1024
-// rows 156 us (177)
+// 128 or 256}.  Measured with 8192 -> 8192: 1024 rows by the first 84 us (by the second 98), 512 by the second 50 (84), 64 by the third 18 (46), 24 by the fourth 13 (18), 400
+// with 8192 -> 512 by the fourth 11.9 (16.7); in groups of 32 1024 rows 156 us by the first (177).  The fourth, with eight waves along k, is for products with one set of weights.
 struct S4TileCost {
     int m, n;
     float fixed, step[3];
 };
-constexpr S4TileCost kS4Tiles[] = {{128, 256, 9.f, {2.3f, 1.5f, 1.17f}}, {128, 128, 9.f, {1.25f, 0.8f, 0.64f}}, {64, 32, 4.f, {0.28f, 0.23f, 0.21f}}};
+constexpr S4TileCost kS4Tiles[] = {{128, 256, 9.f, {2.3f, 1.5f, 1.17f}}, {128, 128, 9.f, {1.25f, 0.8f, 0.64f}}, {64, 32, 4.f, {0.28f, 0.23f, 0.21f}}, {32, 32, 4.f, {0.14f, 0.12f, 0.11f}}};
 constexpr int kS4TileKinds = sizeof(kS4Tiles) / sizeof(kS4Tiles[0]);
 
 struct S4Plan {
@@ -343,8 +343,8 @@ inline S4Plan plan_s4(const LinearS4Args &a, const LinearTuning &tuning)
     float best = 0.f;
     for (int c = 0; c < kS4TileKinds; ++c) {
         const S4TileCost &t = kS4Tiles[c];
-        // (the last one's weight rows are twice as many in a gated layer, for a third more time)
-        const bool wider = c == kS4TileKinds - 1 && a.w2;
+        if (a.w2 && c > 2) continue;
+        const bool wider = a.w2 && c == 2;                 // (the third one's weight rows are twice as many in a gated layer, for a third more time)
         const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + (wider ? 2 : 1) * t.n - 1) / ((wider ? 2 : 1) * t.n));
         const float us = __builtin_ceilf(tiles / 256.f) * (t.fixed + (wider ? 1.3f : 1.f) * (float)steps * t.step[by_group]);
         if (best == 0.f || us < best) {

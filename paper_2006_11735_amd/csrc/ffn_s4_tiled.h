@@ -404,7 +404,8 @@ static hipError_t launch_s4_tiles(const LinearS4Args &a, int tile, hipStream_t s
     switch (tile) {
     case 0: return launch_s4_tile<2, 2, 4, 2, 1, GROUP, false>(a, st);
     case 1: return launch_s4_tile<2, 2, 2, 2, 2, GROUP, false>(a, st);
-    default: return launch_s4_tile<1, 1, 1, 2, 4, GROUP, false>(a, st);
+    case 2: return launch_s4_tile<1, 1, 1, 2, 4, GROUP, false>(a, st);
+    default: return launch_s4_tile<1, 1, 1, 1, 8, GROUP, false>(a, st);
     }
 }
 

@@ -223,6 +223,23 @@ def test_every_kernel(kernel, which, counts, k, n):
         run(counts, k, n, dtype, "silu", gated=True, seed=which + 10, **extra)
 
 
+@pytest.mark.parametrize("which", [0, 1, 2, 3, 5, 9, 10])
+def test_many_experts(kernel, which):
+    kernel(which)
+    g = np.random.default_rng(which)
+    shares = [[1, 0] * 30, [0] * 100 + [1, 1, 0, 1]] if which == 2 else [list(g.integers(0, 4, size=1000)) + [300, 0, 129] + [0] * 21, [0] * 63 + [5, 260, 7] + [0] * 70 + [128]]
+    for counts in shares:
+        rows = int(sum(counts))
+        run([int(c) for c in counts], 96, 40, "f32", "silu", gated=True, index=g.permutation(rows), behind=0, seed=1)
+        run([int(c) for c in counts], 100, 33, "bf16", first=3, behind=4, seed=2)
+
+
+def test_all_positions_are_one_expert_s():
+    for counts in ([0] * 7 + [700] + [0] * 8, [1500] + [0] * 63):
+        run(counts, 256, 136, "f16", "gelu", seed=3)
+        run(counts, 200, 72, "f16", "silu", gated=True, seed=4)
+
+
 @pytest.mark.parametrize("k", [1024, 1025, 2047, 2048, 4096, 4111, 8192, 8208, 16384, 16399, 32768, 32780])
 def test_depths_of_single_tokens(k):
     run([1, 0, 1, 1], k, 21, "f32", seed=k)

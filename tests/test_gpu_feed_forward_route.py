@@ -80,6 +80,14 @@ def test_types_scores_strides(dtype, score, normalise):
     Router(logits_of(90, 60, 4, 40.0), 5, dtype, score, normalise, -0.5).go()
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("experts", [128, 256, 512, 1024])
+@pytest.mark.parametrize("pad,offset", [(0, 1), (1, 0), (7, 3), (8, 8)])
+def test_whole_lanes_of_experts_at_odd_places(dtype, experts, pad, offset):
+    for rows in (5, 90):
+        Router(logits_of(rows, experts, 7), 6, dtype, "softmax", False, 1.0, pad, offset).go()
+
+
 def test_a_negative_stream_of_sigmoids_is_normalised_all_the_same():
     logits = logits_of(50, 40, 5) - 150                # each sigmoid leaves float32
     r = Router(logits, 3, "f32", "sigmoid", True)

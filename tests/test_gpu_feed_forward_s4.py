@@ -196,7 +196,7 @@ def kernel():
 
 
 @pytest.mark.parametrize("which,rows", [(1, 1), (1, 50), (2, 1), (2, 2), (2, 3), (2, 4), (3, 1), (3, 16), (3, 17), (3, 32)] +
-                         [(k, m) for k in (4, 5, 6) for m in (1, 63, 64, 65, 130, 300)])
+                         [(k, m) for k in (4, 5, 6, 7) for m in (1, 31, 32, 33, 63, 64, 65, 130, 300)])
 @pytest.mark.parametrize("k,n", [(16, 16), (64, 7), (300, 96), (512, 260), (1040, 129), (2320, 520)])
 def test_every_kernel(kernel, which, rows, k, n):
     kernel(which)

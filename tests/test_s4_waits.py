@@ -10,7 +10,7 @@ from paper_2006_11735_amd import binding, build
 
 LLVM = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin")
 # (TN, TM, WN, WM, WK): stages by the size of a group
-TILES = [(2, 2, 4, 2, 1), (2, 2, 2, 2, 2), (2, 1, 1, 2, 4), (1, 1, 1, 2, 4)]
+TILES = [(2, 2, 4, 2, 1), (2, 2, 2, 2, 2), (2, 1, 1, 2, 4), (1, 1, 1, 2, 4), (1, 1, 1, 1, 8)]
 
 
 def sizes(tn, tm, wn, wm, wk, group):
