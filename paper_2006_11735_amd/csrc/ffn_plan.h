@@ -329,14 +329,16 @@ struct S4Plan {
     int tile;                      // of LinearKernel::tiled: its place in kS4Tiles
 };
 
-// Up to four rows token by token (1 x 16384 -> 4096: 8.3 us, by the kernel for few rows 16), up to 32 by the kernel for few rows (24 x 8192 -> 8192: 15 us, in tiles 19),
-// the others in tiles; k below 16 and rows gigabytes apart by the plain kernel
+// Up to four rows token by token (1 x 16384 -> 4096: 8.3 us, by the kernel for few rows 16), up to 16 by the kernel for few rows, up to 32 by that or in tiles by what has
+// been measured (24 rows: 4096 -> 4096 7.7 us, in tiles 8.5, 8192 -> 8192 15.3 and 13.3; 32 rows, gated 4096 -> 16384: 33 and 26), the others in tiles; k below 16 and rows
+// gigabytes apart by the plain kernel
 inline S4Plan plan_s4(const LinearS4Args &a, const LinearTuning &tuning)
 {
     const int force = tuning.kernel;
     if (a.M <= 4 && a.K >= 16 && a.K <= 32768 && (force == 0 || force == 2)) return {LinearKernel::tokens, 0};
-    if (a.M <= 32 && a.K >= 16 && (force == 0 || force == 3)) return {LinearKernel::few, 0};
-    if (a.K < 16 || a.ldx > (1 << 22) || (force != 0 && force < 4)) return {LinearKernel::plain, 0};
+    const bool few = a.M <= 32 && a.K >= 16, tiled = a.K >= 16 && a.ldx <= (1 << 22);
+    if (few && (force == 3 || (force == 0 && (a.M <= 16 || !tiled)))) return {LinearKernel::few, 0};
+    if (!tiled || (force != 0 && force < 4)) return {LinearKernel::plain, 0};
     if (force >= 4) return {LinearKernel::tiled, force - 4 < kS4TileKinds ? force - 4 : kS4TileKinds - 1};
     const int steps = (a.K + 127) / 128, by_group = a.group == 32 ? 0 : a.group == 64 ? 1 : 2;
     S4Plan p = {LinearKernel::tiled, 0};
@@ -352,6 +354,12 @@ inline S4Plan plan_s4(const LinearS4Args &a, const LinearTuning &tuning)
             p.tile = c;
         }
     }
+    // The kernel for few rows: a start, and the weights' way (megabytes), which the rows at odd places hold up, or a wave's turns of 128 bytes one after the other.  Tiles take 3 us
+    // more on such rows.  (32 rows, 2001 -> 5461: 9.1 us, in tiles 9.1, gated 16.7 and 12.3.)
+    const bool odd = (((uintptr_t)a.x | (uintptr_t)a.ldx) & 3) != 0;
+    const float mb = (a.w2 ? 2.f : 1.f) * (float)a.N * (float)a.ldw * 1e-6f, way = (odd ? 0.9f : 0.36f) * mb, chain = 1.7f * (float)a.ldw / 1024.f;
+    const float few_us = 4.f + (a.group == 32 ? 1.35f : 1.f) * (way > chain ? way : chain);
+    if (few && force == 0 && few_us < 1.1f * (best + (odd ? 3.f : 0.f))) p.kernel = LinearKernel::few;
     return p;
 }
 
