@@ -1,5 +1,5 @@
 // Products of few 8-bit rows and 4-bit weights (see ffn_s4.hip for the mathematics).  What counts is how fast the weights come in: each is used for 16 * MT rows
-// at most.  A workgroup has 32 outputs of all rows (16 of a gated layer); its eight waves share the k axis, in turns of RB bytes of a weight row (twice as many numbers), and join their sums in
+// at most.  A workgroup has 16 T outputs of all rows (16 of a gated layer, see launch_group); its eight waves share the k axis, in turns of RB bytes of a weight row (twice as many numbers), and join their sums in
 // LDS at the end.  A wave's weights come in whole lines, a turn ahead in registers, and go through LDS, where no other wave reads them, into the order of the matrix
 // instruction: 64 numbers of k, of which lane l has 16 (half (l >> 4) & 1 of block l >> 5).  The rows, which every workgroup reads, come out of the caches, a turn ahead too.
 #include "ffn_s4.h"
@@ -10,7 +10,7 @@ namespace icnn {
 
 namespace {
 
-// Eight waves of 32 rows of weights (both layers' sixteen, where there are two): the rows come from the caches half as often as with sixteen
+// Eight waves of T * 16 rows of weights (both layers' sixteen, where there are two); with 32 of them the rows come from the caches half as often as with 16
 constexpr int NW = 8, RB = 128, PIECES = RB / 16, COPIES = RB / 64, XQ = RB / 32;
 
 // Wait states between the last products and their sums' first reader (see mfma_drain in conv_common.h)
