@@ -714,6 +714,7 @@ int icombine_rows(const icnn_combine_desc *desc, const void *v, const float *gat
  *   igated_linear_s4:  y = v * (the same of up_packed, up_scale and up_bias, without act);   v of gate_packed, gate_scale, gate_bias
  * A group's sum is exact (int32); the sum over the groups is in float32, in an order that depends on the number of rows and on the sizes: the same row in calls of other
  * row counts may differ in its last bits.
+ * An infinite scale gives an infinity or a NaN: a group may be added up in parts.
  * Packed weights: iweights_s4_bytes bytes, 16-byte aligned; row n is ceil(k / 32) blocks of 16 bytes, byte j of a block holds number 32 b + j in its lower and number
  * 32 b + 16 + j in its upper four bits; what is behind k may be anything.  w_scale: scale_dtype [n][ceil(k / group)].
  * y may not overlap another operand but its residual in place.  ceil(rows / 16) * ceil(n / 16) is at most 2^25.

@@ -90,7 +90,7 @@ static hipError_t launch_tokens(const GroupedArgs &a, hipStream_t st)
     constexpr int NWT = KW > 4 ? KW : 4, HALF = OUT / 2 < 1 ? 1 : OUT / 2;
     const int per = (a.l.w2 ? HALF : OUT) * (NWT / KW), blocks_n = (a.l.N + per - 1) / per;
     const long long groups = (long long)a.l.M * blocks_n;
-    if (!fits_launch(groups, 64 * NWT)) return hipErrorInvalidValue;
+    if (!fits_launch(groups, 64 * NWT)) return launch_plain(a, st);
     if (a.l.w2) hipLaunchKernelGGL((grouped_tokens_kernel<C, KW, HALF, true>), dim3((unsigned)groups), dim3(64 * NWT), 0, st, a, blocks_n);
     else hipLaunchKernelGGL((grouped_tokens_kernel<C, KW, OUT, false>), dim3((unsigned)groups), dim3(64 * NWT), 0, st, a, blocks_n);
     return hipGetLastError();

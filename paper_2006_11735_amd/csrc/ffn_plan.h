@@ -322,7 +322,7 @@ struct S4TileCost {
     float fixed, step[3];
 };
 constexpr S4TileCost kS4Tiles[] = {{128, 256, 9.f, {2.3f, 1.5f, 1.17f}}, {128, 128, 9.f, {1.25f, 0.8f, 0.64f}}, {64, 32, 4.f, {0.28f, 0.23f, 0.21f}}, {32, 32, 4.f, {0.14f, 0.12f, 0.11f}}};
-constexpr int kS4TileKinds = sizeof(kS4Tiles) / sizeof(kS4Tiles[0]);
+constexpr int kS4TileKinds = sizeof(kS4Tiles) / sizeof(kS4Tiles[0]), kS4TileThreads = 512;
 
 struct S4Plan {
     LinearKernel kernel;
@@ -339,19 +339,20 @@ inline S4Plan plan_s4(const LinearS4Args &a, const LinearTuning &tuning)
     const bool few = a.M <= 32 && a.K >= 16, tiled = a.K >= 16 && a.ldx <= (1 << 22);
     if (few && (force == 3 || (force == 0 && (a.M <= 16 || !tiled)))) return {LinearKernel::few, 0};
     if (!tiled || (force != 0 && force < 4)) return {LinearKernel::plain, 0};
-    if (force >= 4) return {LinearKernel::tiled, force - 4 < kS4TileKinds ? force - 4 : kS4TileKinds - 1};
     const int steps = (a.K + 127) / 128, by_group = a.group == 32 ? 0 : a.group == 64 ? 1 : 2;
-    S4Plan p = {LinearKernel::tiled, 0};
+    S4Plan p = {LinearKernel::plain, 0};
     float best = 0.f;
-    for (int c = 0; c < kS4TileKinds; ++c) {
+    const int kinds = a.w2 ? 3 : kS4TileKinds, only = force < 4 ? -1 : force - 4 < kinds ? force - 4 : kinds - 1;
+    for (int c = 0; c < kinds; ++c) {
         const S4TileCost &t = kS4Tiles[c];
-        if (a.w2 && c > 2) continue;
+        if (only >= 0 && c != only) continue;
         const bool wider = a.w2 && c == 2;                 // (the third one's weight rows are twice as many in a gated layer, for a third more time)
-        const float tiles = (float)((a.M + t.m - 1) / t.m) * (float)(((a.w2 ? 2ll : 1ll) * a.N + (wider ? 2 : 1) * t.n - 1) / ((wider ? 2 : 1) * t.n));
-        const float us = __builtin_ceilf(tiles / 256.f) * (t.fixed + (wider ? 1.3f : 1.f) * (float)steps * t.step[by_group]);
+        const long long tiles = ((a.M + t.m - 1ll) / t.m) * (((a.w2 ? 2ll : 1ll) * a.N + (wider ? 2 : 1) * t.n - 1) / ((wider ? 2 : 1) * t.n));
+        if (!fits_launch(tiles + 7, kS4TileThreads)) continue;             // (of half a billion rows the first tile's always does)
+        const float us = __builtin_ceilf((float)tiles / 256.f) * (t.fixed + (wider ? 1.3f : 1.f) * (float)steps * t.step[by_group]);
         if (best == 0.f || us < best) {
             best = us;
-            p.tile = c;
+            p = {LinearKernel::tiled, c};
         }
     }
     // The kernel for few rows: a start, and the weights' way (megabytes), which the rows at odd places hold up, or a wave's turns of 128 bytes one after the other.  Tiles take 3 us

@@ -35,7 +35,7 @@ struct S4Tile {
     static constexpr int SCALES = GROUPS * BN * 4, REST = 2 * SCALES + BM * 4, STAGES = 4 * STAGE + REST <= 163840 ? 4 : 3, LDS = STAGES * STAGE + REST;
     static constexpr bool AHEAD = STAGES == 4;             // fragments of the next stage under this one's products
     static constexpr int OUT = GATED ? BN / 2 : BN;
-    static_assert(WM * 32 * OUT * 4 <= STAGES * STAGE && (WK - 1) * BM * BN * 4 <= STAGES * STAGE && LDS <= 163840, "what takes the ring's place");
+    static_assert(WM * 32 * OUT * 4 <= STAGES * STAGE && (WK - 1) * BM * BN * 4 <= STAGES * STAGE && LDS <= 163840 && THREADS == kS4TileThreads, "what takes the ring's place");
 };
 
 }  // namespace
@@ -375,7 +375,6 @@ static hipError_t launch_s4_one(const LinearS4Args &a, hipStream_t st)
     typedef S4Tile<TN, TM, WN, WM, WK, GROUP, GATED> S;
     const int tiles_n = (a.N + S::OUT - 1) / S::OUT, tiles_m = (a.M + S::BM - 1) / S::BM;
     const long long per = ((long long)tiles_n * tiles_m + 7) / 8;
-    if (!fits_launch(per * 8, S::THREADS)) return hipErrorInvalidValue;
     auto *const k = s4_tiled_kernel<TN, TM, WN, WM, WK, GROUP, GATED, DIRECT, WIDE>;
     if (hipError_t e = allow_large_lds((const void *)k)) return e;
     hipLaunchKernelGGL(k, dim3((unsigned)(per * 8)), dim3(S::THREADS), S::LDS, st, a, tiles_n, tiles_m, (int)per);

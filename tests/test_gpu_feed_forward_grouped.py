@@ -244,3 +244,18 @@ def test_all_positions_are_one_expert_s():
 def test_depths_of_single_tokens(k):
     run([1, 0, 1, 1], k, 21, "f32", seed=k)
     run([0, 1, 1, 0], k, 5, "bf16", "silu", gated=True, index=np.array([1, 0]), seed=k)
+
+
+def test_more_outputs_than_a_launch_of_the_kernel_for_single_positions_holds(kernel):
+    kernel(2)
+    rows, k, n = 64, 16, 2 ** 22
+    g = torch.Generator(device="cuda:0").manual_seed(4)
+    x, w = (torch.randint(-128, 128, s, generator=g, device="cuda:0", dtype=torch.int32).to(torch.int8) for s in ((rows, k), (n, k)))
+    one, y = torch.ones(n, device="cuda:0"), torch.zeros((rows, n), device="cuda:0")
+    offsets = torch.tensor([0, rows], dtype=torch.int32, device="cuda:0")
+    B.igrouped_linear_s8(B.grouped_desc(rows=rows, k=k, n=n, experts=1, dtype=B.ICNN_F32), x, one, None, offsets, w, one, None, y)
+    torch.cuda.synchronize()
+    want = torch.zeros_like(y)
+    for i in range(k):                                 # (integers below 2^24: exact)
+        want += x[:, i, None].float() * w[:, i].float()
+    assert (y == want).all()

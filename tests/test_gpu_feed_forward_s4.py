@@ -205,6 +205,24 @@ def test_every_kernel(kernel, which, rows, k, n):
         run(rows, k, n, group, dtype, "silu", gated=True, pads=pads, offset=offset, scales=scales, seed=which + 10)
 
 
+@pytest.mark.parametrize("rows,which", [(2 ** 29, 0), (2 ** 29 - 3, 7)])
+def test_as_many_rows_as_there_may_be(kernel, rows, which):
+    """Whatever tiles one launch does not hold, another kernel has the product"""
+    kernel(which)
+    k, n, some = 16, 5, 70
+    g = torch.Generator(device="cuda:0").manual_seed(3)
+    x = torch.ones((rows, k), dtype=torch.int8, device="cuda:0")
+    x[-some:] = torch.randint(-128, 128, (some, k), generator=g, device="cuda:0").to(torch.int8)
+    numbers = np.random.default_rng(3).integers(-8, 8, size=(n, k))
+    w = torch.from_numpy(packed4(numbers)).to("cuda:0")
+    scale, xs, y = torch.ones((n, 1), dtype=torch.float16, device="cuda:0"), torch.ones(rows, device="cuda:0"), torch.zeros((rows, n), device="cuda:0")
+    B.ilinear_s4(B.linear_s4_desc(rows=rows, k=k, n=n, group=32, dtype=B.ICNN_F32), x, xs, w, scale, None, None, y)
+    torch.cuda.synchronize()
+    want = torch.from_numpy(numbers).double()
+    assert (y[-some:].double().cpu() == x[-some:].double().cpu() @ want.T).all()           # (integers below 2^24)
+    assert (y[:-some] == want.sum(1).float().to("cuda:0")).all()
+
+
 @pytest.mark.parametrize("k", [2047, 2048, 2049, 4095, 4096, 4111, 8192, 8208, 16384, 16399, 32767, 32768, 32780])
 def test_depths_of_single_tokens(k):
     for rows in (1, 2, 4):
