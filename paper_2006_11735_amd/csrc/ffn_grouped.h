@@ -9,15 +9,17 @@ struct Place {
     int expert, m0, end;
 };
 
-// Groups of ROWS positions of one expert each: all of them (the last one of an expert may have fewer), or those with more than half of ROWS, or an expert's rest of up to
-// half of ROWS
-enum Groups { kAll, kWholeOrMost, kRest };
+// Groups of ROWS positions of one expert each: all of them (the last one of an expert may have fewer), or those with more than half of ROWS, or an expert's rest of up
+// to half, and of those the ones of more than a quarter, or of up to a quarter of ROWS
+enum Groups { kAll, kWholeOrMost, kRest, kHalf, kQuarter };
 
 template <int ROWS, Groups KIND>
 __device__ __forceinline__ int groups_among(int positions)
 {
     const int rest = positions % ROWS;
     if (KIND == kRest) return rest > 0 && rest <= ROWS / 2;
+    if (KIND == kHalf) return rest > ROWS / 4 && rest <= ROWS / 2;
+    if (KIND == kQuarter) return rest > 0 && rest <= ROWS / 4;
     return positions / ROWS + (KIND == kAll ? rest > 0 : rest > ROWS / 2);
 }
 
@@ -71,7 +73,7 @@ struct Shares {
                 const int at = __builtin_ctzll(beyond);
                 const int before = __builtin_amdgcn_readlane(up - own, at), first = __builtin_amdgcn_readlane(lo, at);
                 p.end = __builtin_amdgcn_readlane(hi, at);
-                p.m0 = KIND == kRest ? first + (p.end - first) / ROWS * ROWS : first + (slot - before) * ROWS;
+                p.m0 = KIND >= kRest ? first + (p.end - first) / ROWS * ROWS : first + (slot - before) * ROWS;
                 p.expert = p.m0 >= first && p.m0 < p.end ? base + at : -1;     // (always, but where sums of offsets that do not ascend have left 32 bits)
                 return p;
             }

@@ -223,6 +223,17 @@ def test_every_kernel(kernel, which, counts, k, n):
         run(counts, k, n, dtype, "silu", gated=True, seed=which + 10, **extra)
 
 
+@pytest.mark.parametrize("counts", [[256] * 100 + [200] * 28, [256] * 120 + [300, 330, 400, 511, 512, 513], [1000] * 33, [256 * 64, 256 * 64 + 100, 40], [65] * 200 + [130] * 100,
+                                    [250] * 200 + [100, 30] * 20])
+@pytest.mark.parametrize("k", [16, 200, 384, 4000])
+def test_full_turns_of_tiles_and_what_is_beyond_them(kernel, counts, k):
+    kernel(10)
+    g = np.random.default_rng(k)
+    rows = sum(counts)
+    run(counts, k, 300, "f32", seed=1)
+    run(counts, k, 270, "bf16", "silu", gated=True, index=g.integers(0, rows, size=rows), x_rows=rows, seed=2)
+
+
 @pytest.mark.parametrize("which", [0, 1, 2, 3, 5, 9, 10])
 def test_many_experts(kernel, which):
     kernel(which)
