@@ -21,7 +21,7 @@ __global__ __launch_bounds__(WN * WM * 64, waves_per_simd(WN * WM, 32 * (TN * WN
 template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED, bool DIRECT>
 static hipError_t launch_one(const GroupedArgs &a, hipStream_t st)
 {
-    constexpr int BN = 32 * TN * WN / (GATED ? 2 : 1), BM = 32 * TM * WM, LDS = 32 * (TN * WN + TM * WM) * BK * STAGES;
+    constexpr int BN = 32 * TN * WN / (GATED ? 2 : 1), BM = 32 * TM * WM, LDS = 32 * (TN * WN + TM * WM) * BK * STAGES + 8 * BM;
     TiledArgs t = {};
     t.l = a.l;
     t.tiles_n = (a.l.N + BN - 1) / BN;
@@ -136,8 +136,8 @@ template <bool GATED, bool DIRECT, bool EIGHTHS>
 static hipError_t launch_mixed(const GroupedArgs &a, hipStream_t st)
 {
     static_assert(!(GATED && EIGHTHS), "a wave of 32 weight rows has one layer's");
-    constexpr int BN = GATED ? 128 : 256, LDS = 3 * (256 + 128) * 128;
-    static_assert(LDS >= 2 * (256 + 256) * 128 && LDS >= 6 * (128 + 64) * 128, "any size's stages");
+    constexpr int BN = GATED ? 128 : 256, LDS = 3 * (256 + 128) * 128 + 8 * 128;
+    static_assert(LDS >= 2 * (256 + 256) * 128 + 8 * 256 && LDS >= 6 * (128 + 64) * 128 + 8 * 64, "any size's stages and rows");
     TiledArgs t = {};
     t.l = a.l;
     t.tiles_n = (a.l.N + BN - 1) / BN;

@@ -122,6 +122,23 @@ __device__ __forceinline__ void tiled_product(const TiledArgs &ta, const LinearA
         const int m = min(q, a.M - 1 - m0);
         off_x[j] = (unsigned)(indexed ? max(row_of(*ga, m0 + m), 0) : m) * (unsigned)a.ldx + 16 * piece_x[j];
     }
+    // The epilogue's scales of the rows and which rows there are not, behind the stages in LDS: by the index they are two loads one after the other
+    static_assert(NW * 64 >= BM, "a thread a row");
+    float *const row_scales = (float *)(lds + STAGES * STAGE);
+    int *const row_names = (int *)(row_scales + BM), own = threadIdx.x % BM;
+    int own_name = 0;
+    float own_scale = 0.f;
+    if (GROUPED) {
+        const int m = m0 + min(own, a.M - 1 - m0);
+        own_name = indexed ? row_of(*ga, m) : m;
+        own_scale = a.xs[max(own_name, 0)];
+    }
+    auto put_rows = [&]() {
+        if (GROUPED) {
+            row_scales[own] = own_scale;
+            row_names[own] = own_name;
+        }
+    };
     const int first = range * ta.steps_per * BK, steps = min(ta.steps_per, (a.K - first + BK - 1) / BK), end = min(a.K, first + steps * BK);
     // copies FROM .. TO - 1 of step s: of the weights, then of the rows.  Behind the last step nothing but zeros comes.
     auto copy_part = [&](int s, auto from, auto to) {
@@ -213,11 +230,14 @@ __device__ __forceinline__ void tiled_product(const TiledArgs &ta, const LinearA
         for (int s = 0; s < STAGES; ++s)
             if (s < STAGES - 1) copy_part(s, None{}, All{});
             else copy_part(s, None{}, Half{});
+        put_rows();
         FFN_WAIT_VMCNT((STAGES - 2) * LOADS + LOADS / 2);
+        if (GROUPED) FFN_WAIT_LGKM();
     } else {
         times(std::integral_constant<int, AHEAD>{}, [&](auto u) { fetch_step(u, u); });
         put_step(0, None{});
         fetch_step(AHEAD, None{});
+        put_rows();
         FFN_WAIT_LGKM();
     }
     asm volatile("" ::: "memory");
@@ -329,7 +349,7 @@ __device__ __forceinline__ void tiled_product(const TiledArgs &ta, const LinearA
         asm volatile("" ::: "memory");
     };
     // P rows of a thread at a time; the residual of the next ones is on its way
-    const bool with_res = !GATED && a.res;
+    const bool with_res = !GATED && !GROUPED && a.res;
     auto dump = [&](auto j0) {
 #pragma unroll
         for (int j = 0; j < JR; ++j)
@@ -356,15 +376,12 @@ __device__ __forceinline__ void tiled_product(const TiledArgs &ta, const LinearA
         uint8_t *const y0 = (uint8_t *)a.y + ((m0 + q0) * a.ldy + n) * ITEM;
         Eight<DT> ahead[DEPTH][P] = {};
         float xs_ahead[DEPTH][P] = {};
-        bool none[DEPTH][P] = {};                          // (rows whose index names none of x)
         auto fetch = [&](int turn, int to) {
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 const int u = above(turn, p);
-                if (u < last) {
-                    const int from = indexed ? row_of(*ga, m0 + q0 + u) : 0;
-                    xs_ahead[to][p] = indexed ? a.xs[max(from, 0)] : xs0[u];
-                    none[to][p] = from < 0;
+                if (!GROUPED && u < last) {
+                    xs_ahead[to][p] = xs0[u];
                     if (with_res) ahead[to][p] = all ? load_eight<DT>(res0 + u * a.ldr * ITEM, 0) : load_up_to_eight<DT>(res0 + u * a.ldr * ITEM, a.N - n);
                 }
             }
@@ -385,8 +402,8 @@ __device__ __forceinline__ void tiled_product(const TiledArgs &ta, const LinearA
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 res[p] = ahead[slot][p];
-                xs[p] = xs_ahead[slot][p];
-                left_out[p] = none[slot][p];
+                xs[p] = GROUPED ? row_scales[q0 + above(turn, p)] : xs_ahead[slot][p];
+                left_out[p] = GROUPED && row_names[q0 + above(turn, p)] < 0;       // (its index names no row of x)
 #pragma unroll
                 for (int e = 0; e < (GATED ? 4 : 2); ++e)
                     t[p][e] = *(const v4i *)(from + p * PASS * (BN * 4) + (((c0 + (e & 1) + (e & 2) * 4) ^ ((q0 + p * PASS) & 15)) << 4));
@@ -415,7 +432,7 @@ __device__ __forceinline__ void tiled_product(const TiledArgs &ta, const LinearA
                 float out[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) out[e] = v[8 * p + e];
-                if (u < last && !(GROUPED && left_out[p])) {
+                if (u < last && !left_out[p]) {
                     uint8_t *const at = y0 + u * a.ldy * ITEM;
                     if (all) {
                         store_eight<DT>(at, 0, out);
