@@ -300,4 +300,16 @@ __device__ __forceinline__ void finish_four(const LinearArgs &a, const v4i &c, c
         }
 }
 
+// The sums of a wave's lanes up to each, by moves within the vector unit; all lanes have to be there
+__device__ __forceinline__ int sums_up_to(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);         // from 1, 2, 4 and 8 lanes below in sixteen
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);        // lanes 15 and 47 to the sixteen above them
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);        // lane 31 to the upper half
+    return v;
+}
+
 }  // namespace icnn

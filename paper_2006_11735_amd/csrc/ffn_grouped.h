@@ -48,26 +48,18 @@ struct Shares {
             load(base, &lo, &hi);
             all += groups_among<ROWS, KIND>(hi - lo);
         }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
-        return __builtin_amdgcn_readfirstlane(all);
+        return __builtin_amdgcn_readlane(sums_up_to(all), 63);
     }
 
     // The `slot`-th of them, expert by expert
     template <int ROWS, Groups KIND = kAll>
     __device__ __forceinline__ Place place(int slot) const
     {
-        const int lane = threadIdx.x & 63;
         Place p = {-1, 0, 0};
         int lo = lo0, hi = hi0;
         for (int base = 0;;) {
             const int own = groups_among<ROWS, KIND>(hi - lo);
-            int up = own;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int below = __shfl_up(up, d);
-                if (lane >= d) up += below;
-            }
+            const int up = sums_up_to(own);
             const unsigned long long beyond = __ballot(up > slot);
             if (beyond) {
                 const int at = __builtin_ctzll(beyond);

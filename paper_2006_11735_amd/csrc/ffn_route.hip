@@ -109,12 +109,7 @@ __device__ __forceinline__ int scan_counts(int experts, int *first, F &&count)
     int total = 0;
     for (int base = 0; base < experts; base += THREADS) {
         const int own = base + t < experts ? count(base + t) : 0;
-        int up = own;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int below = __shfl_up(up, d);
-            if (lane >= d) up += below;
-        }
+        const int up = sums_up_to(own);
         if (WAVES > 1) {
             if (base) __syncthreads();                     // (the sums of the turn before have been read)
             if (lane == 63) sums[t >> 6] = up;
