@@ -152,7 +152,7 @@ const char *icnn_last_error(void);
  *   "tri_tile"    0 library's choice; 1..4 = the 3x3 + 1x1 + 1x1 kernel at any size, in tiles of 32, 64, 96 or 112 pixels
  *   "ff_kernel"   0 library's choice; products of 8-bit rows, where the shape allows it, by 1 the plain kernel, 2 the one for up to four rows, 3 the one for up to 64
  *                 rows, 4..9 in tiles of 256 x 256, 128 x 256, 128 x 128 (two or one on a compute unit), 64 x 128, 64 x 64 rows x weight rows; those grouped by
- *                 expert so too, 2 position by position (up to 64), 10 in tiles of 256 x 256 and 128 x 256; those with 4-bit weights by 1, 2 and, up to 32
+ *                 expert so too, 2 position by position (up to 64), 10 in tiles of 256 x 256 and smaller ones in one launch; those with 4-bit weights by 1, 2 and, up to 32
  *                 rows, 3 likewise, 4..7 in tiles of 128 x 256, 128 x 128, 64 x 32, 32 x 32
  *   "ff_split"    0 library's choice; 1 their k axis stays whole; 2..16 it is split into up to so many ranges where the shape and the workspace allow
  *   "ksplit"      0, 1 never split the K axis over workgroups (the library's choice); 2..8 that split where it divides the K steps

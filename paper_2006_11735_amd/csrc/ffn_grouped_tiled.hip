@@ -49,8 +49,8 @@ static hipError_t launch_tiles(const GroupedArgs &a, hipStream_t st)
 // 256 x 256 do not fill the chip's 256 compute units once more, those beyond the last time they do may be cut in two of 128 x 256 or in eight of 64 x 128, and so may the
 // rests' tiles of 128 x 256 in four: whatever is expected to end soonest.  In hundredths of a tile's time half of it takes 56 and an eighth `eighth` (8192 -> 8192: 37 us of
 // 163, 1024 -> 8192 12 of 33).  EIGHTHS: from 32 steps of k on (2048 rows, top 2 of 8, 4096 -> 4096 103 us without, 97 with; 4096, top 4 of 32, 2048 -> 2048 108 and 111), but
-// not in gated layers, where a wave needs both layers' rows: 64 rows take 40 there (2048, top 4 of 32, 2048 -> 2048 107 and 113).
-// (4096 rows, top 2 of 8, 8192 -> 4096: 316 us in tiles of one size, 304 in two, 289 in three.)
+// not in gated layers, where a wave needs both layers' rows: 64 rows take 40 there (2048, top 4 of 32, 2048 -> 2048 107 and 113; 98 to 110 by now).
+// (4096 rows, top 2 of 8, 8192 -> 4096: 316 us in tiles of one size, 304 in two, 289 in three; the latter 276 to 286 by now.)
 constexpr int kMostCut = 1024;     // workgroups that cuts may add
 
 template <bool GATED, bool DIRECT, bool EIGHTHS>
@@ -161,7 +161,7 @@ static hipError_t launch_mixed_of(const GroupedArgs &a, hipStream_t st)
     return a.l.K > 31 * 128 ? launch_mixed<false, DIRECT, true>(a, st) : launch_mixed<false, DIRECT, false>(a, st);
 }
 
-// (the cases in the order of kTiles, and the one of two sizes)
+// (the cases in the order of kTiles, and the one of several sizes)
 hipError_t launch_grouped_tiled(const GroupedArgs &a, int tile, hipStream_t st)
 {
     static_assert(kTileKinds == 6, "a case a tile");

@@ -230,7 +230,7 @@ inline bool grouped_tiled_takes(const GroupedArgs &a) { return a.l.K >= 16 && a.
 inline bool grouped_few_takes(const GroupedArgs &a) { return a.l.K >= 16 && a.l.ldw <= (1 << 26); }
 inline bool grouped_tokens_takes(const GroupedArgs &a) { return a.l.K >= 16 && a.l.K <= 32768 && a.l.M <= 64; }
 
-// (beside the sizes of kTiles: tiles of 256 x 256 and of 128 x 256 in one launch)
+// (beside the sizes of kTiles: tiles of 256 x 256 and smaller ones in one launch)
 constexpr int kMixedTiles = kTileKinds;
 
 struct GroupedPlan {
