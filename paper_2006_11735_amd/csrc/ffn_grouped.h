@@ -9,20 +9,6 @@ struct Place {
     int expert, m0, end;
 };
 
-// Groups of ROWS positions of one expert each: all of them (the last one of an expert may have fewer), or those with more than half of ROWS, or an expert's rest of up
-// to half, and of those the ones of more than a quarter, or of up to a quarter of ROWS
-enum Groups { kAll, kWholeOrMost, kRest, kHalf, kQuarter };
-
-template <int ROWS, Groups KIND>
-__device__ __forceinline__ int groups_among(int positions)
-{
-    const int rest = positions % ROWS;
-    if (KIND == kRest) return rest > 0 && rest <= ROWS / 2;
-    if (KIND == kHalf) return rest > ROWS / 4 && rest <= ROWS / 2;
-    if (KIND == kQuarter) return rest > 0 && rest <= ROWS / 4;
-    return positions / ROWS + (KIND == kAll ? rest > 0 : rest > ROWS / 2);
-}
-
 // The experts' positions as a wave asks for them, all of its lanes together: lane l has the first 64 experts' l-th, so that a second question does not wait for memory again.
 // The answers are the same in all lanes.  Whatever the offsets hold, the positions are in [0, M).
 struct Shares {

@@ -98,7 +98,7 @@ static hipError_t launch_tokens(const GroupedArgs &a, hipStream_t st)
 
 hipError_t launch_grouped(const GroupedArgs &a, hipStream_t st)
 {
-    const GroupedPlan plan = plan_grouped(a, linear_tuning(), step_factor(a.l));
+    const GroupedPlan plan = plan_grouped_launch(a, linear_tuning());
     switch (plan.kernel) {
     case LinearKernel::tokens:
         if (a.l.K <= 1024) return launch_tokens<1, 1, 4>(a, st);

@@ -295,6 +295,126 @@ inline GroupedPlan plan_grouped(const GroupedArgs &a, const LinearTuning &tuning
     return p;
 }
 
+// What a launch does: the plan for its operands' addresses
+inline GroupedPlan plan_grouped_launch(const GroupedArgs &a, const LinearTuning &tuning) { return plan_grouped(a, tuning, step_factor(a.l)); }
+
+// Groups of ROWS positions of one expert each: all of them (the last one of an expert may have fewer), or those with more than half of ROWS, or an expert's rest of up
+// to half, and of those the ones of more than a quarter, or of up to a quarter of ROWS
+enum Groups { kAll, kWholeOrMost, kRest, kHalf, kQuarter };
+
+template <int ROWS, Groups KIND>
+constexpr int groups_among(int positions)
+{
+    const int rest = positions % ROWS;
+    if (KIND == kRest) return rest > 0 && rest <= ROWS / 2;
+    if (KIND == kHalf) return rest > ROWS / 4 && rest <= ROWS / 2;
+    if (KIND == kQuarter) return rest > 0 && rest <= ROWS / 4;
+    return positions / ROWS + (KIND == kAll ? rest > 0 : rest > ROWS / 2);
+}
+
+// Tile `slot` of tiles_m x tiles_n: eight rows of tiles, column after column, so that what an XCD has at one time shares its weights and rows
+constexpr void tile_at(int slot, int tiles_m, int tiles_n, int *tm, int *tn)
+{
+    const int rows = 8, panel = slot / (rows * tiles_n), in_panel = slot - panel * rows * tiles_n, left = tiles_m - panel * rows, high = left < rows ? left : rows;
+    *tn = in_panel / high;
+    *tm = panel * rows + in_panel - *tn * high;
+}
+
+// Tiles of several sizes in one launch: an expert's positions in groups of 256, what is left of them in one of 256 or, up to 128 or 64, of so many.  Where the tiles of
+// 256 x 256 do not fill the chip's 256 compute units once more, those beyond the last time they do may be cut in two of 128 x 256 or in eight of 64 x 128, and so may the
+// rests' tiles of 128 x 256 in four: whatever is expected to end soonest.  In hundredths of a tile's time half of it takes 56 and an eighth `eighth` (8192 -> 8192: 37 us of
+// 163, 1024 -> 8192 12 of 33).  EIGHTHS: from 32 steps of k on (2048 rows, top 2 of 8, 4096 -> 4096 103 us without, 97 with; 4096, top 4 of 32, 2048 -> 2048 108 and 111), but
+// not in gated layers, where a wave needs both layers' rows: 64 rows take 40 there (2048, top 4 of 32, 2048 -> 2048 107 and 113; 98 to 110 by now).
+// (4096 rows, top 2 of 8, 8192 -> 4096: 316 us in tiles of one size, 304 in two, 289 in three; the latter 276 to 286 by now.)
+constexpr int kMixedRows = 256, kMostCut = 1024;           // workgroups that cuts may add
+
+// Workgroups of such a launch, a multiple of 8: a group's tiles, or twice as many of a rest's; what cuts add; up to 7 / 8 of a workgroup for each XCD and size
+template <bool EIGHTHS>
+constexpr long long mixed_blocks(long long positions, int experts, int tiles_n)
+{
+    const long long groups = positions / kMixedRows + (positions < experts ? positions : experts), rests = groups - positions / kMixedRows;
+    return (((EIGHTHS ? groups + rests : groups) * tiles_n + (EIGHTHS ? kMostCut : 256)) / 8 + 4) * 8;
+}
+
+// What a workgroup of it has: of the groups of kind `from` the `slot`-th, `down` rows further on, and the n-th tile of its columns; rows 256, 128 or 64; 0: nothing
+struct MixedTile {
+    int rows, slot, n, down;
+    Groups from;
+};
+
+// groups, rests, small: how many of kWholeOrMost, of kRest (kHalf with EIGHTHS) and of kQuarter there are.  tiles_n, tiles8_n: tiles of 256 and of 64 rows beside each other
+template <bool EIGHTHS>
+constexpr MixedTile mixed_tile(int groups, int rest_groups, int small_groups, int tiles_n, int tiles8_n, int steps, unsigned block)
+{
+    constexpr Groups REST = EIGHTHS ? kHalf : kRest;
+    constexpr int ROWS = kMixedRows, PARTS = 8, HALF = 56;
+    const int eighth = 22 + 120 / steps, whole = groups * tiles_n, rests = rest_groups * tiles_n, beyond = whole & 255, small = EIGHTHS ? small_groups * tiles8_n : 0;
+    // Of the tiles beyond the last full turn `in2` are cut in halves or `in8` in eighths, of the rests' halves `in4` in quarters
+    int in2 = 0, in8 = 0, in4 = 0, least = 0x7fffffff;
+    auto option = [&](int h, int e, int r) {
+        if (h + e * (PARTS - 1) + r * (PARTS / 2 - 1) > kMostCut) return;
+        const int bigs = beyond - h - e, halves = rests + 2 * h - r, eighths = small + e * PARTS + r * (PARTS / 2), more = halves - (256 - bigs);
+        const int first = bigs ? 100 : 0, then = halves ? (first > HALF ? first : HALF) + HALF * (((more > 0 ? more : 0) + 255) / 256) : first;
+        const int all = (100 * bigs + HALF * halves + eighth * eighths) / 256 + (eighths ? eighth / 2 : 0), end = then > all ? then : all;
+        if (end < least) {
+            least = end;
+            in2 = h;
+            in8 = e;
+            in4 = r;
+        }
+    };
+    option(0, 0, 0);
+    option(beyond, 0, 0);
+    if (EIGHTHS) {
+        option(0, beyond, 0);
+        option(0, beyond, rests);
+        option(beyond, 0, rests);
+    }
+    const int bigs = whole - in2 - in8, halves = rests + 2 * in2 - in4, eighths = small + in8 * PARTS + in4 * (PARTS / 2);
+    const int x = (int)(block & 7), per_big = (bigs + 7) / 8, per_half = (halves + 7) / 8, per_eighth = (eighths + 7) / 8;
+    const int i = (int)(block >> 3), i2 = i - per_big, i8 = i2 - per_half;
+    MixedTile t = {0, 0, 0, 0, kWholeOrMost};
+    if (i2 < 0) {
+        const int unit = x * per_big + i;
+        if (unit >= bigs) return t;
+        tile_at(unit, groups, tiles_n, &t.slot, &t.n);
+        t.rows = ROWS;
+    } else if (i8 < 0) {
+        const int unit = x * per_half + i2, of_rests = unit - 2 * in2;
+        if (unit >= halves) return t;
+        if (of_rests < 0) {
+            tile_at(bigs + unit / 2, groups, tiles_n, &t.slot, &t.n);
+            t.down = ROWS / 2 * (unit & 1);
+        } else {
+            t.slot = of_rests / tiles_n;
+            t.n = of_rests - t.slot * tiles_n;
+            t.from = REST;
+        }
+        t.rows = ROWS / 2;
+    } else if (EIGHTHS) {
+        const int unit = x * per_eighth + i8, of_rests = unit - in8 * PARTS, of_small = of_rests - in4 * (PARTS / 2);
+        if (i8 >= per_eighth || unit >= eighths) return t;
+        if (of_small < 0) {                                // 64 rows and half the columns of a tile
+            const int part = of_rests < 0 ? unit % PARTS : of_rests % (PARTS / 2), tile = of_rests < 0 ? bigs + unit / PARTS : of_rests / (PARTS / 2);
+            if (of_rests < 0) {
+                tile_at(tile, groups, tiles_n, &t.slot, &t.n);
+            } else {
+                t.slot = tile / tiles_n;
+                t.n = tile - t.slot * tiles_n;
+                t.from = REST;
+            }
+            t.down = ROWS / 4 * (part / 2);
+            t.n = 2 * t.n + part % 2;
+        } else {
+            t.slot = of_small / tiles8_n;
+            t.n = of_small - t.slot * tiles8_n;
+            t.from = kQuarter;
+        }
+        if (t.n < tiles8_n) t.rows = ROWS / 4;
+    }
+    return t;
+}
+
 // What one launch holds by any kernel: 16 x 16 outputs a wave
 constexpr long long kMostTiles = 1 << 25;
 inline bool grouped_fits(long long positions, int experts, int n) { return grouped_slots(positions, experts, 16) <= kMostTiles / ((n + 15ll) / 16); }

@@ -71,15 +71,6 @@ __device__ __forceinline__ void drain(v16i (&acc)[TN][TM])
 
 }  // namespace
 
-// Tile `slot` of tiles_m x tiles_n: eight rows of tiles, column after column, so that what an XCD has at one time shares its weights and rows
-__device__ __forceinline__ void tile_at(int slot, int tiles_m, int tiles_n, int *tm, int *tn)
-{
-    constexpr int GROUP = 8;
-    const int panel = slot / (GROUP * tiles_n), in_panel = slot - panel * GROUP * tiles_n, high = min(GROUP, tiles_m - panel * GROUP);
-    *tn = in_panel / high;
-    *tm = panel * GROUP + in_panel - *tn * high;
-}
-
 // A tile: the workgroup's of all tiles of `a`, and of their k axis's ranges.  GROUPED: rows m0_of .. of an expert's (a.M is where they end; see ffn_grouped.hip), x's being
 // what the index says, and outputs n0_of ..; k is whole.
 template <int TN, int TM, int WN, int WM, int BK, int STAGES, bool GATED, bool DIRECT, bool GROUPED>
