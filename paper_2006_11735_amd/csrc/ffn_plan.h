@@ -28,9 +28,9 @@ constexpr bool fits_launch(long long groups, int threads) { return groups <= 0xf
 // How much longer a step along k is where rows go through registers: with k whole 64 x 5456 -> 2048 (rows at multiples of 16) 15.2 us,
 // 5464 (of 8) 15.8, 5461 19.8; 4096 x 2048 -> 8192 in 256 x 256 tiles 87 us, 2047 112
 constexpr float kStepFactors[] = {1.f, 1.2f, 1.7f};         // rows at multiples of 16 bytes, of 4, anywhere
-inline float step_factor(const LinearArgs &a)
+inline float step_factor(const LinearArgs &a, long long expert_stride = 0)
 {
-    const unsigned at = (unsigned)((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.w2) | (unsigned)(a.ldx | a.ldw);
+    const unsigned at = (unsigned)((uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.w2) | (unsigned)(a.ldx | a.ldw | expert_stride);
     return kStepFactors[at & 3 ? 2 : (at | (unsigned)a.K) & 15 ? 1 : 0];
 }
 
@@ -295,8 +295,8 @@ inline GroupedPlan plan_grouped(const GroupedArgs &a, const LinearTuning &tuning
     return p;
 }
 
-// What a launch does: the plan for its operands' addresses
-inline GroupedPlan plan_grouped_launch(const GroupedArgs &a, const LinearTuning &tuning) { return plan_grouped(a, tuning, step_factor(a.l)); }
+// What a launch does: the plan for its operands' addresses, every expert's
+inline GroupedPlan plan_grouped_launch(const GroupedArgs &a, const LinearTuning &tuning) { return plan_grouped(a, tuning, step_factor(a.l, a.expert_stride)); }
 
 // Groups of ROWS positions of one expert each: all of them (the last one of an expert may have fewer), or those with more than half of ROWS, or an expert's rest of up
 // to half, and of those the ones of more than a quarter, or of up to a quarter of ROWS

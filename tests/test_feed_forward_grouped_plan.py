@@ -85,6 +85,18 @@ def test_every_launch_with_4_bit_weights_fits(lib, gated, k):
     assert taken > 1000
 
 
+def test_experts_at_odd_places_are_planned_as_what_their_copies_are(lib):
+    """An expert's weights start at multiples of 16 bytes only if the stride between experts is one: else the copies go through registers, as of weights at such an address"""
+    changed = 0
+    for gated, rows, k, n in itertools.product((0, 1), (40, 100, 300, 600, 1000, 1500, 3000, 8000), (512, 1024, 4096, 8192), (512, 1024, 2048, 4096)):
+        for off in (16, 8, 4, 2, 1):
+            plan, moved, aligned = (grouped(lib, rows, k, n, 8, gated, **place)[:2] for place in (dict(expert_stride=n * k + off), dict(w=off), {}))
+            assert plan == moved, (gated, rows, k, n, off)
+            assert off != 16 or plan == aligned
+            changed += plan != aligned
+    assert changed > 20
+
+
 def mixed(lib, offsets, rows, n, steps, gated, eighths):
     """(pieces of 64 x 128 that no workgroup has, that several have, workgroups outside, workgroups with something)"""
     out = (ctypes.c_longlong * 4)()
