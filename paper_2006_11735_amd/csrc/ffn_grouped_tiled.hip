@@ -108,8 +108,8 @@ hipError_t launch_grouped_tiled(const GroupedArgs &a, int tile, hipStream_t st)
     case kMixedTiles:
         return tiled_direct(a.l, a.expert_stride) ? launch_mixed_of<true>(a, st) : launch_mixed_of<false>(a, st);
     default:
-        if (a.l.w2) return launch_tiles<2, 1, 1, 2, 128, 4>(a, st);
-        return tiled_direct(a.l, a.expert_stride) ? launch_one<1, 1, 2, 2, 128, 4, false, true>(a, st) : launch_one<1, 1, 2, 2, 128, 2, false, false>(a, st);
+        if (tiled_direct(a.l, a.expert_stride)) return a.l.w2 ? launch_one<2, 1, 1, 2, 128, 4, true, true>(a, st) : launch_one<1, 1, 2, 2, 128, 4, false, true>(a, st);
+        return a.l.w2 ? launch_one<2, 1, 1, 2, 128, 2, true, false>(a, st) : launch_one<1, 1, 2, 2, 128, 2, false, false>(a, st);
     }
 }
 

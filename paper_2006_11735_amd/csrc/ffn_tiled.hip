@@ -50,8 +50,8 @@ hipError_t launch_tiled_linear(const LinearArgs &a, const TilePlan &p, hipStream
     case 3: return launch_tiles<2, 2, 2, 2, 128, 4>(a, p.splits, st);
     case 4: return launch_tiles<2, 1, 2, 2, 128, 3>(a, p.splits, st);
     default:                                               // (four waves where gate and up need not be in one: 24 x 256 -> 8192 3.6 us, by two waves 4.2)
-        if (a.w2) return launch_tiles<2, 1, 1, 2, 128, 4>(a, p.splits, st);
-        return tiled_direct(a, 0) ? launch_one<1, 1, 2, 2, 128, 4, false, true>(a, p.splits, st) : launch_one<1, 1, 2, 2, 128, 2, false, false>(a, p.splits, st);
+        if (tiled_direct(a, 0)) return a.w2 ? launch_one<2, 1, 1, 2, 128, 4, true, true>(a, p.splits, st) : launch_one<1, 1, 2, 2, 128, 4, false, true>(a, p.splits, st);
+        return a.w2 ? launch_one<2, 1, 1, 2, 128, 2, true, false>(a, p.splits, st) : launch_one<1, 1, 2, 2, 128, 2, false, false>(a, p.splits, st);
     }
 }
 
