@@ -135,6 +135,7 @@ __device__ __forceinline__ void few_product(const LinearArgs &a, const GroupedAr
             asm volatile("" ::: "memory");
         } else {
             put(t);
+            asm volatile("" ::: "memory");                 // (other lanes of the wave read it: the hardware keeps a wave's order, the compiler knows of one lane's own addresses only)
             fetch(t + 1);
             const int k0 = (wave + t * NW) * RB;
             if (k0 + RB > a.K) {

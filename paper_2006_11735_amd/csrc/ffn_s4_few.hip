@@ -24,6 +24,9 @@ __device__ __forceinline__ void drain(v4i (&acc)[N])
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(acc[i]));
 }
 
+// What a wave's lanes write to LDS others of it read: the hardware keeps a wave's order, the compiler knows of one lane's own addresses only
+__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
+
 }  // namespace
 
 template <int MT, int T, int GROUP, bool GATED, bool WIDE>
@@ -94,6 +97,7 @@ __global__ __launch_bounds__(NW * 64, 2) void s4_few_kernel(const LinearS4Args a
     // (a piece of the rows is loaded for the next turn as soon as it has been used: one set of registers)
     auto turn = [&](int t, auto more) {
         put(t);
+        in_order();
         if (more) fetch(t + 1);
         const int k0 = (wave + t * NW) * RB * 2;
         if (k0 + 2 * RB > a.K) {
@@ -144,6 +148,7 @@ __global__ __launch_bounds__(NW * 64, 2) void s4_few_kernel(const LinearS4Args a
             }
             if (more) load_rows(t + 1, q);
         }
+        in_order();
     };
     if (mine) {
         fetch(0);
