@@ -47,6 +47,8 @@ def quantize_weights_s4(w, group=128, scale_dtype=torch.float16):
     """(packed uint8, scales [n][groups]) of floating weights on the GPU: 4-bit numbers with the step max|w| / 7 for each `group` numbers of a row."""
     if w.dim() != 2 or w.dtype not in _CODES or scale_dtype not in _CODES:
         raise ValueError("weights are [n][k] numbers of float32, float16 or bfloat16, and scales of these types: got %s of %s, %s" % (tuple(w.shape), w.dtype, scale_dtype))
+    if group not in (32, 64, 128, 256):
+        raise ValueError("group is 32, 64, 128 or 256: got %s" % (group,))
     n, k = w.shape
     if w.stride(1) != 1 or w.stride(0) < k:
         w = w.contiguous()
