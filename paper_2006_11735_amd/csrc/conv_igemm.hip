@@ -18,8 +18,8 @@
 //   conv_greg_kernel  any cin / alignment / raw-picture input: tiles are staged
 //                     through registers (double-buffered LDS).
 #include "conv_common.h"
+#include "once_per_device.h"
 
-#include <mutex>
 #include <type_traits>
 
 namespace icnn {
@@ -626,18 +626,13 @@ __global__ __launch_bounds__(256) void conv_greg_kernel(const ConvArgs a)
 }
 
 // ------------------------------------------------------------------ dispatch
-// More than 64 KiB of dynamic LDS has to be allowed once per kernel function.
+// More than 64 KiB of dynamic LDS has to be allowed once per kernel function, on each device.
 hipError_t allow_large_lds(const void *kernel)
 {
-    static std::mutex lock;
-    static const void *done[256];                    // (more kernels than the library has; beyond, the attribute is set anew)
-    static int n = 0;
-    std::lock_guard<std::mutex> g(lock);
-    for (int i = 0; i < n; ++i)
-        if (done[i] == kernel) return hipSuccess;
-    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    if (e == hipSuccess && n < 256) done[n++] = kernel;
-    return e;
+    static OncePerDevice once;
+    int device = 0;
+    if (hipError_t e = hipGetDevice(&device)) return e;
+    return (hipError_t)once(kernel, device, [&] { return (int)hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); });
 }
 
 template <int BM, int BP, int WAVES_M, int WAVES_P>

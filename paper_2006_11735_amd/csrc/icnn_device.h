@@ -260,7 +260,7 @@ struct Tuning {
     int keep = 0;          // 3x3 layers of 64 channels with their weights kept in registers: 1 every layer that kernel accepts, 2 none
     int flat = 0;          // kernel with register-fed weights: 1 every layer whose shape it accepts, 2 none
     int tri_tile = 0;      // 3x3 + 1x1 + 1x1 kernel: 1..4 = tiles of 32, 64, 96 or 112 pixels
-    int ff_kernel = 0;     // products of 8-bit rows: 1 plain kernel, 2 token by token, 3 few rows, 4..9 a tile size, where the shape allows
+    int ff_kernel = 0;     // products of 8-bit rows: 1 plain kernel, 2 token by token, 3 few rows, 4..10 a tile size, where the shape allows
     int ff_split = 0;      // their k axis in tiles: 1 whole, 2..16 in up to so many ranges
     int ksplit = 0;        // 0, 1 the K axis stays whole (the library's choice); 2..8 this split where it divides the K steps
 };
@@ -272,7 +272,7 @@ hipError_t launch_conv(const ConvArgs &a, bool vec_in, bool direct_ok, hipStream
 // bytes of split-K partial accumulators launch_conv would use for this layer when given a workspace (0: no split)
 size_t conv_split_bytes(const ConvArgs &a, bool direct_ok);
 hipError_t launch_conv_dual(const ConvArgs &a, const ProjArgs &q, hipStream_t st);
-hipError_t allow_large_lds(const void *kernel);   // > 64 KiB of dynamic LDS, once per kernel function
+hipError_t allow_large_lds(const void *kernel);   // > 64 KiB of dynamic LDS, once per kernel function and device
 bool conv_lat_applies(const ConvArgs &a);
 bool conv_lat_before_flat(const ConvArgs &a);
 hipError_t launch_conv_lat(const ConvArgs &a, hipStream_t st);
