@@ -675,6 +675,7 @@ int iroute_top(const icnn_route_desc *desc, const void *logits, int32_t *expert,
  * [experts][n].  Rows of y that belong to no expert (in front of offsets[0], behind offsets[experts], and those whose index is not in [0, x_rows)) are left as they
  * were.  Offsets have to ascend; of others only so much holds that nothing but y's rows is written and nothing outside the operands is read.
  * y may not overlap another operand: ICNN_E_UNSUPPORTED.  (rows / 16 + min(rows, experts)) * ceil(n / 16) is at most 2^25.
+ * With an index many positions are fast only while x_rows * x_stride is below 2 GiB: beyond, the same call takes about eight times as long.
  */
 typedef struct {
     int64_t rows;                  /* positions, y's rows: 0 <= rows <= 2^31 - 2^16 */
@@ -714,13 +715,13 @@ int icombine_rows(const icnn_combine_desc *desc, const void *v, const float *gat
  *   igated_linear_s4:  y = v * (the same of up_packed, up_scale and up_bias, without act);   v of gate_packed, gate_scale, gate_bias
  * A group's sum is exact (int32); the sum over the groups is in float32, in an order that depends on the number of rows and on the sizes: the same row in calls of other
  * row counts may differ in its last bits.
- * An infinite scale gives an infinity or a NaN: a group may be added up in parts.
+ * An infinite scale gives an infinity or a NaN: a group may be added up in parts.  Scales are taken over 16 in float32: one below 2^-122 loses its last bits.
  * Packed weights: iweights_s4_bytes bytes, 16-byte aligned; row n is ceil(k / 32) blocks of 16 bytes, byte j of a block holds number 32 b + j in its lower and number
  * 32 b + 16 + j in its upper four bits; what is behind k may be anything.  w_scale: scale_dtype [n][ceil(k / group)].
  * y may not overlap another operand but its residual in place.  ceil(rows / 16) * ceil(n / 16) is at most 2^25.
  *
- * iquantize_weights_s4 makes both of floating weights, once: scale = max|w| / 7 of a group, rounded to its type; number = w / scale to nearest, ties to even,
- * in [-7, 7].  A group of zeros, or whose scale is rounded to zero, has scale 0 and numbers 0; one that holds a NaN or an infinity, or whose scale leaves its type, scale
+ * iquantize_weights_s4 makes both of floating weights, once: scale = max|w| / 7 of a group, rounded to its type; number = w / scale, of the rounded scale, to nearest, ties
+ * to even, in [-7, 7].  A group of zeros, or whose scale is rounded to zero, has scale 0 and numbers 0; one that holds a NaN or an infinity, or whose scale leaves its type, scale
  * NaN and numbers 0.
  */
 typedef struct {

@@ -131,7 +131,7 @@ __device__ __forceinline__ void few_product(const LinearArgs &a, const GroupedAr
         if (DIRECT) {
             copy(t + DEPTH - 1);                           // into the stage that the last turn has read (its fragments have left it)
             asm volatile("" ::: "memory");
-            FFN_WAIT_VMCNT(XL + COPIES);                   // all but the next turn's rows and weights (tests/test_few_waits.py counts them in the built kernels)
+            FFN_WAIT_VMCNT(XL + COPIES);                   // all but the next turn's rows and weights (tests/test_few_waits.py and test_grouped_waits.py count them in the built kernels)
             asm volatile("" ::: "memory");
         } else {
             put(t);

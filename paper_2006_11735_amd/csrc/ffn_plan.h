@@ -224,7 +224,8 @@ inline long long grouped_slots(long long positions, int experts, int rows)
     return positions / rows + (positions < experts ? positions : experts);
 }
 
-// Operands' offsets in a tile within 2 GiB: rows of an index lie anywhere in x
+// Operands' offsets in a tile within 2 GiB: rows of an index lie anywhere in x.  (Beyond, the kernel for few rows has them: 16384 positions of 8 experts, 8192 -> 4096, with an x of
+// 260000 rows 558 us, of 300000 4580.)
 inline bool grouped_rows_near(const GroupedArgs &a) { return a.index ? a.l.ldx <= (0x7ff00000ll / (a.x_rows > 0 ? a.x_rows : 1)) : a.l.ldx <= (1 << 22); }
 inline bool grouped_tiled_takes(const GroupedArgs &a) { return a.l.K >= 16 && a.l.ldw <= (1 << 22) && grouped_rows_near(a); }
 inline bool grouped_few_takes(const GroupedArgs &a) { return a.l.K >= 16 && a.l.ldw <= (1 << 26); }
@@ -449,7 +450,7 @@ struct S4Plan {
     int tile;                      // of LinearKernel::tiled: its place in kS4Tiles
 };
 
-// Up to four rows token by token (1 x 16384 -> 4096: 8.3 us, by the kernel for few rows 16), up to 16 by the kernel for few rows, up to 32 by that or in tiles by what has
+// (All on operands that no cache holds.)  Up to four rows token by token (1 x 16384 -> 4096: 8.3 us, by the kernel for few rows 16), up to 16 by the kernel for few rows, up to 32 by that or in tiles by what has
 // been measured (24 rows: 4096 -> 4096 7.7 us, in tiles 8.5, 8192 -> 8192 15.3 and 13.3; 32 rows, gated 4096 -> 16384: 33 and 26), the others in tiles; k below 16 and rows
 // gigabytes apart by the plain kernel
 inline S4Plan plan_s4(const LinearS4Args &a, const LinearTuning &tuning)

@@ -150,7 +150,8 @@ class FeedForward:
 
 class ExpertsFeedForward:
     """The same with experts: each token's row goes through the `top` experts that its router logits pick.  Weights are [experts, hidden, width] (gate and up) and
-    [experts, width, hidden] (down), the router's [experts, width]; all are brought to 8 bits.  `stream` and `update` are the [rows, width] buffers a program reads
+    [experts, width, hidden] (down), the router's [experts, width]; all are brought to 8 bits, the router's too: of logits that are closer than its steps another expert may
+    be picked than by its weights as they were (iroute_top takes any logits of a program that has its own).  `stream` and `update` are the [rows, width] buffers a program reads
     and writes; run(n) takes their first n rows through the block, in place."""
 
     def __init__(self, gamma, w_router, w_gate, w_up, w_down, *, rows, top, act="silu", score="softmax", normalise=True, scale=1.0, b_router=None, b_gate=None, b_up=None,
