@@ -92,7 +92,8 @@ __device__ __forceinline__ int four_bits(float w, float scale)
     return (int)fminf(fmaxf(t, -7.f), 7.f);
 }
 
-// Weights to 4 bits: a thread has a block of 32 numbers, the group / 32 threads of a group are next to each other in a wave.
+// Weights to 4 bits: a thread has a block of 32 numbers, the group / 32 threads of a group are next to each other in a wave.  Bound by its loads, a number at a time, the lanes'
+// 64 or 128 bytes apart: 16384 x 4096 in bfloat16 255 to 261 us, in float32 2450; a program does it once.
 //   scale = max|w| / 7 of the group, rounded to its type; number = w / scale to nearest, ties to even, in [-7, 7]
 __global__ __launch_bounds__(256) void quantize_s4_kernel(const QuantizeS4Args a, int per_row, long long units)
 {
