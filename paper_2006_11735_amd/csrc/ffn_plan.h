@@ -1,4 +1,5 @@
-// How products of 8-bit rows are launched: by which kernel, in which tiles, in how many ranges of k.  Host arithmetic alone, so that it can be tested without a GPU.
+// How products of 8-bit rows are launched: by which kernel, in which tiles, in how many ranges of k, and which tile a workgroup has.  Arithmetic alone, the host's and a kernel's,
+// so that it can be tested without a GPU.
 #pragma once
 #include <stddef.h>
 #include <stdint.h>
